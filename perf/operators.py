@@ -172,7 +172,13 @@ def _fill4(case, nbytes, gen):
 
 
 class _State:
-    pass
+    """Inputs and what a program keeps; closes the pool, and the batch with it, when it is
+    dropped."""
+
+    def __del__(self):
+        kv = getattr(self, "kv", None)
+        if kv is not None:
+            kv.close()
 
 
 def _inputs(case, seed):
