@@ -19,7 +19,8 @@
  *
  *   pool   [num_layers][num_blocks][2 (K,V)][num_kv_heads][block_tokens][head_dim]
  *          elements of 1 (fp8 e4m3) or 2 (fp16, bf16) bytes.  One (layer,
- *          block) "chunk" of C = 2*H*T*D*elem bytes is contiguous.
+ *          block) "chunk" of C = 2*H*T*D*elem bytes is contiguous.  (A 4-bit
+ *          pool has its own chunk: see AQUA_INT4.)
  *   image  of one sequence with block table bt[0..n): layer-major
  *          [num_layers][n][C]; image chunk (l, i) is pool chunk (l, bt[i]).
  *          Images of a multi-sequence call are packed one after another
@@ -96,8 +97,18 @@ enum {
     AQUA_ERR_STATE = -6      /* pool unusable after a latched HIP failure */
 };
 
-/* Element types.  Only the byte width matters to the copy. */
-enum { AQUA_F16 = 1, AQUA_BF16 = 2, AQUA_FP8_E4M3 = 3 };
+/* Element types.  Only the byte width matters to the copy.
+ *
+ * AQUA_INT4 holds 32 consecutive values of a token's key or value (a group;
+ * head_dim is a multiple of 32) as 4-bit codes with a scale and a base, both
+ * fp16: code c stands for the fp16 nearest to base + (16 + c) * scale.  5 bits
+ * a value.  A chunk is 2*H*T*D*5/8 bytes, a multiple of 16:
+ *   codes [2][H][T][D/2 bytes]; of 8 consecutive values e0..e7, in one
+ *         little-endian 32-bit word, e0 e2 e4 e6 are in bits 0-3, 4-7, 8-11,
+ *         12-15 and e1 e3 e5 e7 in bits 16-19 ... 28-31 (so that a shift and a
+ *         mask leave two neighbours in the two halves of a register);
+ *   pairs [2][H][T][D/32] of {scale, base}, behind all codes of the chunk. */
+enum { AQUA_F16 = 1, AQUA_BF16 = 2, AQUA_FP8_E4M3 = 3, AQUA_INT4 = 4 };
 
 /* Offload targets.  DEVICE: device memory on the pool's GPU (a carved-out
  * HBM region standing in for a scale-up peer's memory).  HOST: page-locked
@@ -532,6 +543,127 @@ AQUA_API aqua_status aqua_cfs_partition(const aqua_cfs_request* requests,
                                         uint32_t num_requests, const aqua_cfs_params* params,
                                         uint32_t* batch_index, uint32_t* batch_tokens,
                                         uint32_t* batch_size, uint64_t* blocks_taken);
+
+/* ---- Operators on the pool: what a model does with it between two swaps.
+ *
+ * A batch describes one step of a serving engine: for each sequence its block
+ * table, the tokens of its context and how many of those, the last ones, are
+ * new in this step.  aqua_kv_batch_set checks it on the host and takes it to
+ * the device once; the calls of all layers then use it:
+ *   aqua_kv_append   writes the new tokens' keys and values into the pool,
+ *                    rotating the keys (and the queries) on the way;
+ *   aqua_kv_attend   causal attention of the new tokens over the pool.
+ * The new tokens of all sequences are rows of the caller's tensors, packed in
+ * sequence order: token i of sequence s is row sum_{r<s} new_r + i and stands at
+ * position context_s - new_s + i of its sequence.  Rows behind the last
+ * sequence's are neither read nor written.
+ *
+ * Ordering: these calls run on the caller's stream like the caller's own
+ * kernels.  They take no ticket, and the library puts no wait between them and
+ * swaps: order them with streams, events, aqua_stream_wait (before the first
+ * that reads a block being swapped in) and the like.  A batch's calls, replays
+ * of graphs that captured them among them, share its device tables and its
+ * split sums: those that may overlap in time need a batch each, or one stream.
+ *
+ * Capture: aqua_kv_append and aqua_kv_attend may be captured into a graph.  The
+ * graph uses whatever the batch was last set to before each replay (on the
+ * replay's stream, or ordered before it), so one graph serves every step;
+ * its launches are as wide as the batch's limits, so keep those near.  A
+ * captured append must be given a rotation table of as many rows as the
+ * longest context that a replay will meet: rows behind the table are not
+ * rotated but left unwritten.  aqua_kv_batch_set is refused on a stream that
+ * is being captured.
+ *
+ * Limits: block_tokens a power of two from 4 to 1024; head_dim 64, 128 or 256;
+ * num_q_heads a multiple of the pool's num_kv_heads, at most 65536; a context of
+ * at most 2^30 tokens. */
+typedef struct aqua_kv_batch* aqua_kv_batch_t;
+
+typedef struct {
+    uint32_t num_q_heads; /* query heads; head h reads KV head h / (num_q_heads / H) */
+    uint32_t max_seqs;
+    uint32_t max_tokens;  /* new tokens of all sequences together */
+    uint32_t max_blocks;  /* table entries of all sequences together */
+} aqua_kv_batch_desc;
+
+/* Allocates the batch's device tables and workspace and its pinned staging
+ * memory.  AQUA_ERR_INVALID for a pool or limits outside those above.  The
+ * batch keeps the pool's shape and memory address, and not the pool. */
+AQUA_API aqua_status aqua_kv_batch_create(aqua_kv_pool_t pool, const aqua_kv_batch_desc* desc,
+                                          aqua_kv_batch_t* out);
+
+/* Waits for the device and frees the batch.  Graphs that captured its calls
+ * must not be replayed afterwards. */
+AQUA_API aqua_status aqua_kv_batch_destroy(aqua_kv_batch_t batch);
+
+/* Sets the step.  Tables as in aqua_swap_out; context_tokens[s] counts the new
+ * ones too and may be anything up to what the table holds.  All arrays are
+ * host memory and read before the call returns; the tables reach the device in
+ * stream order.  The host blocks only if four earlier sets are still in flight.
+ *   AQUA_ERR_INVALID    null pointer, offsets that decrease, more new tokens
+ *                       than context, a context over 2^30, a stream in capture
+ *   AQUA_ERR_CAPACITY   more sequences, tokens or table entries than the
+ *                       batch's limits, or a context longer than its table
+ *   AQUA_ERR_RANGE      a block id < 0 or >= num_blocks
+ * After a failure the batch is as it was set before. */
+AQUA_API aqua_status aqua_kv_batch_set(aqua_kv_batch_t batch, uint32_t num_seqs,
+                                       const int32_t* block_ids, const uint64_t* seq_offsets,
+                                       const uint32_t* context_tokens,
+                                       const uint32_t* new_tokens, void* stream);
+
+/* The tensors of a step's append.  All are device memory of the pool's GPU,
+ * 16-byte aligned, [tokens][heads][D] with D and heads contiguous and `..._stride`
+ * elements (a multiple of 8, at least heads * D) from token to token. */
+typedef struct {
+    const void* k;        /* [tokens][H][D] */
+    const void* v;        /* [tokens][H][D] */
+    const void* q;        /* [tokens][num_q_heads][D], or NULL: no queries */
+    void* q_out;          /* rotated queries; may be q itself, with its stride */
+    uint64_t k_stride, v_stride, q_stride, q_out_stride;
+    int32_t dtype;        /* of k, v, q and q_out: AQUA_F16 or AQUA_BF16 */
+    int32_t interleaved;  /* rotated pairs: 0: (j, j + rope_dim/2), 1: (2j, 2j + 1) */
+    const float* rope;    /* [rope_rows][rope_dim]: position p's row holds cos of
+                             pairs 0..rope_dim/2-1, then sin; NULL: no rotation */
+    uint32_t rope_rows;
+    uint32_t rope_dim;    /* rotated part of a head, its first elements: a
+                             multiple of 16, at most D */
+    float k_scale, v_scale; /* fp8 pools: stored is value / scale, finite and > 0;
+                             1 for the other pools */
+} aqua_kv_append_args;
+
+/* Writes the new tokens of the batch into `layer` of the pool, rotated and rounded
+ * once from fp32 to the pool's type: to nearest even; e4m3 saturates at 448;
+ * AQUA_INT4 clamps to +-16384, then scale = (max - min) / 15 and
+ * base = min - 16 * scale of the group (rounded to fp16 in turn) and
+ * code = round((value - base) / scale) - 16, kept within 0..15; a NaN makes its
+ * group NaN.  A 16-bit pool takes tensors of its own type, an fp8 or 4-bit pool
+ * both.  AQUA_ERR_INVALID for tensors other than described, overlapping q and q_out
+ * that are not the same, or a rotation table that is shorter than the longest
+ * context; AQUA_ERR_DUPLICATE when two tokens of the batch go to blocks
+ * that another table of the batch holds too (a shared prefix's blocks can be
+ * read, but its last block has to be copied before one of its owners appends). */
+AQUA_API aqua_status aqua_kv_append(aqua_kv_batch_t batch, uint32_t layer,
+                                    const aqua_kv_append_args* args, void* stream);
+
+typedef struct {
+    const void* q;        /* [tokens][num_q_heads][D], strided and aligned as above */
+    void* out;            /* the same shape; must not overlap q */
+    float* lse;           /* [tokens][num_q_heads] log of the softmax's sum, or NULL */
+    uint64_t q_stride, out_stride;
+    int32_t dtype;        /* of q and out: AQUA_F16 or AQUA_BF16 */
+    float scale;          /* of the scores, usually 1 / sqrt(D); finite */
+    float k_scale, v_scale; /* fp8 pools: what a stored value is multiplied with */
+} aqua_kv_attend_args;
+
+/* out = softmax(scale * k_scale * q k^T) v * v_scale over the tokens up to and
+ * including each query's own position in `layer` of the pool: what aqua_kv_append
+ * has written there, or a swap-in brought.  Whatever stands in the pool behind a
+ * context, or at positions that a query must not see, has no influence, NaN
+ * and infinity included.  Sums and statistics are fp32; the weights are
+ * rounded to the 16-bit type that the matrix instructions take.  Results do not
+ * depend on the order in which workgroups run. */
+AQUA_API aqua_status aqua_kv_attend(aqua_kv_batch_t batch, uint32_t layer,
+                                    const aqua_kv_attend_args* args, void* stream);
 
 #ifdef __cplusplus
 }

@@ -29,7 +29,7 @@ AQUA_ERR_CAPACITY = -4
 AQUA_ERR_HIP = -5
 AQUA_ERR_STATE = -6
 
-AQUA_F16, AQUA_BF16, AQUA_FP8_E4M3 = 1, 2, 3
+AQUA_F16, AQUA_BF16, AQUA_FP8_E4M3, AQUA_INT4 = 1, 2, 3, 4
 AQUA_TARGET_DEVICE, AQUA_TARGET_HOST = 0, 1
 AQUA_HOST_ZERO_COPY, AQUA_HOST_STAGED = 0, 1
 AQUA_LINK_RUNTIME, AQUA_LINK_AUTO = -1, -2
@@ -45,6 +45,8 @@ EXPORTS = (
     "aqua_swap_space_create", "aqua_swap_space_destroy", "aqua_swap_alloc", "aqua_swap_free",
     "aqua_swap_locate", "aqua_swap_reclaim", "aqua_swap_restore", "aqua_swap_usage",
     "aqua_hbm_yardstick", "aqua_swap_noalloc",
+    "aqua_kv_batch_create", "aqua_kv_batch_destroy", "aqua_kv_batch_set", "aqua_kv_append",
+    "aqua_kv_attend",
 )
 
 
@@ -85,6 +87,27 @@ class aqua_cfs_params(ctypes.Structure):
     _fields_ = [("batch_tokens", ctypes.c_uint32), ("decode_slots", ctypes.c_uint32),
                 ("block_tokens", ctypes.c_uint32), ("reserved", ctypes.c_uint32),
                 ("capacity_blocks", ctypes.c_uint64)]
+
+
+class aqua_kv_batch_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_uint32) for n in (
+        "num_q_heads", "max_seqs", "max_tokens", "max_blocks")]
+
+
+class aqua_kv_append_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "q", "q_out")] + \
+        [(n, ctypes.c_uint64) for n in ("k_stride", "v_stride", "q_stride", "q_out_stride")] + \
+        [("dtype", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+         ("rope", ctypes.c_void_p), ("rope_rows", ctypes.c_uint32),
+         ("rope_dim", ctypes.c_uint32), ("k_scale", ctypes.c_float),
+         ("v_scale", ctypes.c_float)]
+
+
+class aqua_kv_attend_args(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("q_stride", ctypes.c_uint64), ("out_stride", ctypes.c_uint64),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float)]
 
 
 class AquaError(RuntimeError):
@@ -138,6 +161,11 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     L.aqua_swap_usage.argtypes = [P] + [ctypes.POINTER(u64)] * 4
     L.aqua_hbm_yardstick.argtypes = [i32, P, P, u64, P]
     L.aqua_swap_noalloc.argtypes = [P, i32, u32, P, P, P, u64, P, i32, P, ctypes.POINTER(u64)]
+    L.aqua_kv_batch_create.argtypes = [P, ctypes.POINTER(aqua_kv_batch_desc), ctypes.POINTER(P)]
+    L.aqua_kv_batch_destroy.argtypes = [P]
+    L.aqua_kv_batch_set.argtypes = [P, u32, P, P, P, P, P]
+    L.aqua_kv_append.argtypes = [P, u32, ctypes.POINTER(aqua_kv_append_args), P]
+    L.aqua_kv_attend.argtypes = [P, u32, ctypes.POINTER(aqua_kv_attend_args), P]
     L.aqua_status_str.argtypes = [i32]
     L.aqua_status_str.restype = ctypes.c_char_p
     for n in EXPORTS:
@@ -345,6 +373,30 @@ def aqua_swap_usage(space):
     return (st, *[x.value for x in v])
 
 
+def aqua_kv_batch_create(pool, desc: aqua_kv_batch_desc):
+    h = ctypes.c_void_p()
+    st = load().aqua_kv_batch_create(pool, ctypes.byref(desc), ctypes.byref(h))
+    return st, h.value
+
+
+def aqua_kv_batch_destroy(batch) -> int:
+    return load().aqua_kv_batch_destroy(batch)
+
+
+def aqua_kv_batch_set(batch, num_seqs, block_ids, seq_offsets, context_tokens, new_tokens,
+                      stream) -> int:
+    return load().aqua_kv_batch_set(batch, num_seqs, block_ids, seq_offsets, context_tokens,
+                                    new_tokens, stream)
+
+
+def aqua_kv_append(batch, layer: int, args: aqua_kv_append_args, stream) -> int:
+    return load().aqua_kv_append(batch, layer, ctypes.byref(args), stream)
+
+
+def aqua_kv_attend(batch, layer: int, args: aqua_kv_attend_args, stream) -> int:
+    return load().aqua_kv_attend(batch, layer, ctypes.byref(args), stream)
+
+
 # -- torch-facing wrapper ------------------------------------------------------
 
 class RawBuffer:
@@ -421,7 +473,7 @@ class KVPool:
         if st != AQUA_OK:
             raise AquaError(st, "aqua_kv_pool_create")
         self.handle = h
-        self._spaces = []      # swap spaces on this pool, closed before it
+        self._spaces = []      # swap spaces and batches on this pool, closed before it
         self._held = {}        # ticket -> the tensors its call names, until it completes
         self._prune_at = 64    # prune completed entries when this many are held
 
@@ -631,6 +683,157 @@ class SwapSpace:
             self.pool._spaces.remove(self)
             if st != AQUA_OK:
                 raise AquaError(st, "aqua_swap_space_destroy")
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+
+_DTYPES = {torch.float16: AQUA_F16, torch.bfloat16: AQUA_BF16}
+
+
+class KVBatch:
+    """One step's sequences on a pool, and the operators of its layers (see
+    aqua_kv_batch_create): ``set`` once a step, then ``append`` and ``attend`` for
+    every layer.  Tensors are [tokens, heads, head_dim] device tensors of one 16-bit
+    type, their heads contiguous, the new tokens of all sequences packed in
+    sequence order.  Closed with its pool at the latest."""
+
+    def __init__(self, pool: "KVPool", num_q_heads: int, max_seqs: int, max_tokens: int,
+                 max_blocks: int):
+        st, h = aqua_kv_batch_create(
+            pool.handle, aqua_kv_batch_desc(num_q_heads, max_seqs, max_tokens, max_blocks))
+        if st != AQUA_OK:
+            raise AquaError(st, "aqua_kv_batch_create")
+        self.handle = h
+        self.pool = pool
+        self.num_q_heads = num_q_heads
+        self.max_tokens = max_tokens
+        self.tokens = 0
+        pool._spaces.append(self)
+
+    def set(self, tables, context, new, stream=None) -> None:
+        """``tables`` as for swaps; ``context``: tokens of each sequence, the new ones
+        among them; ``new``: how many of them are new."""
+        ids, offs = _csr(tables)
+        ctx, fresh = (np.ascontiguousarray(x, dtype=np.int64) for x in (context, new))
+        if not len(ctx) == len(fresh) == len(offs) - 1 or \
+                (len(ctx) and (min(ctx.min(), fresh.min()) < 0 or ctx.max() >= 1 << 32)):
+            raise AquaError(AQUA_ERR_INVALID, "aqua_kv_batch_set")
+        ctx32, fresh32 = ctx.astype(np.uint32), np.minimum(fresh, (1 << 32) - 1).astype(np.uint32)
+        st = aqua_kv_batch_set(self.handle, len(ctx), _addr(ids), _addr(offs), _addr(ctx32),
+                               _addr(fresh32), _stream_handle(stream))
+        if st != AQUA_OK:
+            raise AquaError(st, "aqua_kv_batch_set")
+        self.tokens = int(fresh.sum())
+
+    def _rows(self, t: torch.Tensor, heads: int, what: str) -> int:
+        """The row stride of a tensor that a call may name, after the checks that need
+        its shape (the library sees an address)."""
+        D = self.pool.desc.head_dim
+        capturing = t.is_cuda and torch.cuda.is_current_stream_capturing()
+        rows = self.max_tokens if capturing else self.tokens
+        if (t.dim() != 3 or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != D
+                or not t.is_cuda or (t.numel() and (t.stride(2) != 1 or
+                                                    (heads > 1 and t.stride(1) != D)))):
+            raise AquaError(AQUA_ERR_INVALID, what)
+        # (A single row's stride says nothing.)
+        return t.stride(0) if t.shape[0] > 1 else heads * D
+
+    def _empty(self, q: torch.Tensor) -> torch.Tensor:
+        return torch.empty(q.shape, dtype=q.dtype, device=q.device)
+
+    @staticmethod
+    def _used(stream, *tensors) -> None:
+        """Tensors of torch's allocator that another than the current stream uses are
+        not handed out again before it is done with them."""
+        if stream is None or isinstance(stream, int):
+            return
+        if stream.cuda_stream != torch.cuda.current_stream(stream.device).cuda_stream:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
+
+    def append(self, layer: int, k: torch.Tensor, v: torch.Tensor,
+               q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+               rope: Optional[torch.Tensor] = None, interleaved: bool = False,
+               k_scale: float = 1.0, v_scale: float = 1.0,
+               stream=None) -> Optional[torch.Tensor]:
+        """aqua_kv_append.  ``rope``: float32 [positions, rotated part of a head], cosines
+        and then sines.  Returns the rotated queries (``q_out``, which may be ``q``
+        itself, or a new tensor), None without ``q``."""
+        name, H = "aqua_kv_append", self.pool.desc.num_kv_heads
+        dtype = _DTYPES.get(k.dtype)
+        if dtype is None or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+            raise AquaError(AQUA_ERR_INVALID, name)
+        a = aqua_kv_append_args(k=k.data_ptr(), v=v.data_ptr(), k_stride=self._rows(k, H, name),
+                                v_stride=self._rows(v, H, name), dtype=dtype,
+                                interleaved=int(bool(interleaved)), k_scale=k_scale,
+                                v_scale=v_scale)
+        if q is not None:
+            a.q_stride = self._rows(q, self.num_q_heads, name)
+            if q_out is None:
+                q_out = self._empty(q)
+            if q_out.dtype != q.dtype:
+                raise AquaError(AQUA_ERR_INVALID, name)
+            a.q_out_stride = self._rows(q_out, self.num_q_heads, name)
+            a.q, a.q_out = q.data_ptr(), q_out.data_ptr()
+        elif q_out is not None:
+            raise AquaError(AQUA_ERR_INVALID, name)
+        if rope is not None:
+            if rope.dtype != torch.float32 or rope.dim() != 2 or not rope.is_contiguous() \
+                    or not rope.is_cuda:
+                raise AquaError(AQUA_ERR_INVALID, name)
+            a.rope, a.rope_rows, a.rope_dim = rope.data_ptr(), rope.shape[0], rope.shape[1]
+        st = aqua_kv_append(self.handle, layer, a, _stream_handle(stream))
+        if st != AQUA_OK:
+            raise AquaError(st, name)
+        self._used(stream, k, v, q, q_out, rope)
+        return q_out
+
+    def attend(self, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None,
+               lse=None, scale: Optional[float] = None, k_scale: float = 1.0,
+               v_scale: float = 1.0, stream=None):
+        """aqua_kv_attend.  ``scale`` is 1 / sqrt(head_dim) unless given.  ``lse``: True, or
+        a contiguous float32 tensor [tokens, query heads] to fill; then (out, lse) is
+        returned, else out."""
+        name = "aqua_kv_attend"
+        dtype = _DTYPES.get(q.dtype)
+        if dtype is None:
+            raise AquaError(AQUA_ERR_INVALID, name)
+        stride = self._rows(q, self.num_q_heads, name)
+        if out is None:
+            out = self._empty(q)
+        if out.dtype != q.dtype:
+            raise AquaError(AQUA_ERR_INVALID, name)
+        if lse is True:
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        elif lse is False:
+            lse = None
+        if lse is not None and (lse.dtype != torch.float32 or lse.dim() != 2
+                                or lse.shape[0] < self.tokens
+                                or lse.shape[1] != self.num_q_heads or not lse.is_contiguous()):
+            raise AquaError(AQUA_ERR_INVALID, name)
+        a = aqua_kv_attend_args(
+            q=q.data_ptr(), out=out.data_ptr(), lse=None if lse is None else lse.data_ptr(),
+            q_stride=stride, out_stride=self._rows(out, self.num_q_heads, name), dtype=dtype,
+            scale=self.pool.desc.head_dim ** -0.5 if scale is None else scale,
+            k_scale=k_scale, v_scale=v_scale)
+        st = aqua_kv_attend(self.handle, layer, a, _stream_handle(stream))
+        if st != AQUA_OK:
+            raise AquaError(st, name)
+        self._used(stream, q, out, lse)
+        return out if lse is None else (out, lse)
+
+    def close(self) -> None:
+        if getattr(self, "handle", None):
+            st = aqua_kv_batch_destroy(self.handle)
+            self.handle = None
+            self.pool._spaces.remove(self)
+            if st != AQUA_OK:
+                raise AquaError(st, "aqua_kv_batch_destroy")
 
     def __enter__(self):
         return self

@@ -30,9 +30,9 @@ CORE_LIB = os.path.join(PKG, "libaqua_core.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
-HIP_SOURCES = ["aqua_core.cpp", "cfs.cpp", "swap_kernels.hip", "link_engine.hip",
-               "aqua_capi.hip"]
-CORE_SOURCES = ["aqua_core.cpp", "core_testapi.cpp"]
+HIP_SOURCES = ["aqua_core.cpp", "cfs.cpp", "kv_plan.cpp", "swap_kernels.hip", "link_engine.hip",
+               "aqua_capi.hip", "kv_append.hip", "kv_rows.hip", "kv_tiles.hip", "kv_capi.hip"]
+CORE_SOURCES = ["aqua_core.cpp", "core_testapi.cpp", "kv_plan.cpp", "kv_testapi.cpp"]
 
 # Packed fp32 instructions are switched off for every device compile.
 HIP_FLAGS = [

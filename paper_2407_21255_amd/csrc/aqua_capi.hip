@@ -19,6 +19,7 @@
 #include "aqua.h"
 #include "aqua_core.h"
 #include "link_engine.h"
+#include "pool_view.h"
 #include "swap_kernels.h"
 
 namespace {
@@ -1299,6 +1300,9 @@ aqua_status swap_move(aqua_swap_space* s, int from,
 
 }  // namespace
 
+aqua::PoolView aqua::view_of(const aqua_kv_pool* pool) {
+    return {pool->shape, pool->device, pool->base};
+}
 
 extern "C" {
 

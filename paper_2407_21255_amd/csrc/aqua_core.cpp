@@ -7,13 +7,15 @@ namespace aqua {
 
 namespace {
 
-uint64_t elem_bytes(int32_t dtype) {
+uint64_t elem_bits(int32_t dtype) {
     switch (dtype) {
         case AQUA_F16:
         case AQUA_BF16:
-            return 2;
+            return 16;
         case AQUA_FP8_E4M3:
-            return 1;
+            return 8;
+        case AQUA_INT4:
+            return 5;  // a 4-bit code, and 32 bits of scale and base for 32 of them
         default:
             return 0;
     }
@@ -23,7 +25,7 @@ uint64_t elem_bytes(int32_t dtype) {
 
 aqua_status make_shape(const aqua_kv_desc* d, Shape* out) {
     if (!d || !out) return AQUA_ERR_INVALID;
-    const uint64_t e = elem_bytes(d->dtype);
+    const uint64_t e = elem_bits(d->dtype);
     if (!d->num_layers || !d->num_blocks || !d->num_kv_heads ||
         !d->block_tokens || !d->head_dim || !e)
         return AQUA_ERR_INVALID;
@@ -33,7 +35,8 @@ aqua_status make_shape(const aqua_kv_desc* d, Shape* out) {
     if (d->num_kv_heads > 65536 || d->block_tokens > 65536 || d->head_dim > 65536)
         return AQUA_ERR_INVALID;
     const unsigned __int128 C = (unsigned __int128)2 * d->num_kv_heads *
-                                d->block_tokens * d->head_dim * e;
+                                d->block_tokens * d->head_dim * e / 8;
+    if (d->dtype == AQUA_INT4 && d->head_dim % 32) return AQUA_ERR_INVALID;
     if (C > kMaxChunkBytes) return AQUA_ERR_INVALID;
     if ((unsigned __int128)d->num_layers * d->num_blocks * C > kMaxBytes)
         return AQUA_ERR_INVALID;
@@ -44,7 +47,7 @@ aqua_status make_shape(const aqua_kv_desc* d, Shape* out) {
     s.T = d->block_tokens;
     s.D = d->head_dim;
     s.dtype = d->dtype;
-    s.C = 2ull * s.H * s.T * s.D * e;
+    s.C = 2ull * s.H * s.T * s.D * e / 8;
     if (s.C % 16) return AQUA_ERR_INVALID;
     s.pool_bytes = (uint64_t)s.L * s.N * s.C;
     *out = s;

@@ -16,7 +16,8 @@
 namespace aqua {
 
 // Pool geometry.  One (layer, block) chunk of the pool
-// [L][N][2][H][T][D] is C = 2*H*T*D*elem contiguous bytes.
+// [L][N][2][H][T][D] is C = 2*H*T*D*elem contiguous bytes (5 bits an element
+// in a 4-bit pool).
 struct Shape {
     uint32_t L = 0, N = 0, H = 0, T = 0, D = 0;
     int32_t dtype = 0;
@@ -29,7 +30,8 @@ constexpr uint64_t kMaxChunkBytes = 1ull << 30;
 constexpr uint64_t kMaxBytes = 1ull << 62;
 
 // Fills *out from a descriptor; AQUA_ERR_INVALID for a zero dimension, an
-// unknown dtype, or a chunk that is not a multiple of 16 bytes.
+// unknown dtype, a chunk that is not a multiple of 16 bytes, or a 4-bit pool
+// whose head_dim is no multiple of its groups of 32.
 aqua_status make_shape(const aqua_kv_desc* d, Shape* out);
 
 // One swap call as the caller described it.

@@ -1,0 +1,208 @@
+// kv_plan.cpp -- validation and work split of the operators on the pool (host
+// only).
+#include "kv_plan.h"
+
+#include <algorithm>
+
+namespace aqua {
+
+namespace {
+
+uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+
+struct Split {
+    uint32_t columns, step, fewest, target, most_slots;
+};
+
+// Tokens of a part so that all items of a kernel together make about `target`
+// workgroups.
+uint64_t part_tokens(uint64_t work, const Split& sp) {
+    const uint64_t n = ceil_div(ceil_div(work, sp.target), sp.step) * sp.step;
+    return std::max<uint64_t>(n, sp.fewest);
+}
+
+// Tokens that the columns of a tile see at most.
+uint32_t tile_end(const KvSeq& q, uint32_t G, uint32_t columns, uint32_t tile) {
+    const uint64_t last = std::min<uint64_t>((uint64_t)(tile + 1) * columns,
+                                             (uint64_t)G * q.fresh) - 1;
+    return q.context - q.fresh + (uint32_t)(last / G) + 1;
+}
+
+}  // namespace
+
+aqua_status kv_limits(const Shape& s, const aqua_kv_batch_desc* d, KvLimits* out) {
+    if (!d || !out) return AQUA_ERR_INVALID;
+    if (s.T < 4 || s.T > 1024 || (s.T & (s.T - 1))) return AQUA_ERR_INVALID;
+    if (s.D != 64 && s.D != 128 && s.D != 256) return AQUA_ERR_INVALID;
+    if (!d->num_q_heads || d->num_q_heads > 65536 || d->num_q_heads % s.H)
+        return AQUA_ERR_INVALID;
+    if (!d->max_seqs || !d->max_tokens || !d->max_blocks) return AQUA_ERR_INVALID;
+    if (d->max_seqs > (1u << 24) || d->max_tokens > (1u << 28) || d->max_blocks > (1u << 28))
+        return AQUA_ERR_INVALID;
+    KvLimits m;
+    m.shape = s;
+    m.q_heads = d->num_q_heads;
+    m.seqs = d->max_seqs;
+    m.tokens = d->max_tokens;
+    m.blocks = d->max_blocks;
+    m.group = m.q_heads / s.H;
+    const uint64_t G = m.group, H = s.H;
+    // Items of whole contexts: a sequence's columns round up to a tile.  Items
+    // that splitting adds: at most `target` workgroups.
+    const uint64_t busy = std::min(m.seqs, m.tokens);
+    const uint64_t wide = std::min<uint64_t>(busy, G * m.tokens / (kRowsMostColumns + 1));
+    const uint32_t tc = tile_columns(s.D);
+    const uint64_t rows = busy + std::min<uint64_t>(G * m.tokens / kRowColumns,
+                                                    busy * kRowsMostColumns / kRowColumns);
+    // (A single token's heads may be more columns than kRowsMostColumns; they go to
+    // the tiles kernel, whose items are fewer.)
+    const uint64_t tiles = wide ? wide + G * m.tokens / tc : 0;
+    // Slots: a split item has at least two parts of half a part's tokens each,
+    // so splitting makes at most twice the target.
+    const uint64_t row_slots = 2 * kRowsTarget / H + 2;
+    const uint64_t tile_slots = tiles ? (2 * kTilesTarget / H + 2) * (tc / kRowColumns) : 0;
+    const uint64_t most_rows = rows + 2 * kRowsTarget / H + 2;
+    const uint64_t most_tiles = tiles ? tiles + 2 * kTilesTarget / H + 2 : 0;
+    const uint64_t joins = (row_slots + tile_slots) / 2;
+    if (most_rows * H > 0x7fffffffull || most_tiles * H > 0x7fffffffull ||
+        joins * H * 4 > 0x7fffffffull || (row_slots + tile_slots) * H > 0x7fffffffull)
+        return AQUA_ERR_INVALID;
+    m.rows = (uint32_t)most_rows;
+    m.tiles = (uint32_t)most_tiles;
+    m.joins = (uint32_t)joins;
+    m.slots = (uint32_t)(row_slots + tile_slots);
+    *out = m;
+    return AQUA_OK;
+}
+
+aqua_status kv_plan(const KvLimits& lim, uint32_t num_seqs, const int32_t* ids,
+                    const uint64_t* offs, const uint32_t* context, const uint32_t* fresh,
+                    KvPlan* plan) {
+    if (!plan) return AQUA_ERR_INVALID;
+    const uint32_t T = lim.shape.T, N = lim.shape.N, H = lim.shape.H, G = lim.group;
+    if (num_seqs && (!offs || !context || !fresh)) return AQUA_ERR_INVALID;
+    if (num_seqs && offs[0] != 0) return AQUA_ERR_INVALID;
+    for (uint32_t s = 0; s < num_seqs; ++s)
+        if (offs[s + 1] < offs[s] || fresh[s] > context[s] || context[s] > kMostContext)
+            return AQUA_ERR_INVALID;
+    const uint64_t entries = num_seqs ? offs[num_seqs] : 0;
+    if (entries && !ids) return AQUA_ERR_INVALID;
+    if (num_seqs > lim.seqs || entries > lim.blocks) return AQUA_ERR_CAPACITY;
+    uint64_t tokens = 0;
+    for (uint32_t s = 0; s < num_seqs; ++s) {
+        if (ceil_div(context[s], T) > offs[s + 1] - offs[s]) return AQUA_ERR_CAPACITY;
+        tokens += fresh[s];
+    }
+    if (tokens > lim.tokens) return AQUA_ERR_CAPACITY;
+    uint32_t bad = 0;
+    for (uint64_t i = 0; i < entries; ++i) bad |= (uint32_t)ids[i] >= N;
+    if (bad) return AQUA_ERR_RANGE;
+
+    plan->seqs.clear();
+    plan->rows.clear();
+    plan->tiles.clear();
+    plan->joins.clear();
+    plan->tokens.clear();
+    plan->entries = (uint32_t)entries;
+    plan->longest = 0;
+
+    // Tokens, and whether an append may write them: a block that is written
+    // stands in one place of one table only.
+    if (plan->mark.size() != N || plan->epoch == 0xffffffffu) {
+        plan->mark.assign(N, 0);
+        plan->epoch = 0;
+    }
+    const uint64_t epoch = (uint64_t)++plan->epoch << 32;
+    plan->append_ok = true;
+    uint32_t row = 0;
+    for (uint32_t s = 0; s < num_seqs; ++s) {
+        plan->seqs.push_back({(uint32_t)offs[s], context[s], fresh[s], row});
+        row += fresh[s];
+        if (!fresh[s]) continue;
+        plan->longest = std::max(plan->longest, context[s]);
+        for (uint32_t p = context[s] - fresh[s]; p < context[s]; ++p)
+            plan->tokens.push_back({(uint32_t)ids[offs[s] + p / T], p});
+        for (uint32_t b = (context[s] - fresh[s]) / T; b <= (context[s] - 1) / T; ++b) {
+            uint64_t& m = plan->mark[ids[offs[s] + b]];
+            if ((m & ~0xffffffffull) == epoch) plan->append_ok = false;
+            m = epoch | (offs[s] + b);
+        }
+    }
+    for (uint32_t s = 0; s < num_seqs && plan->append_ok; ++s)
+        for (uint64_t i = offs[s]; i < offs[s] + ceil_div(context[s], T); ++i) {
+            const uint64_t m = plan->mark[ids[i]];
+            if ((m & ~0xffffffffull) == epoch && m != (epoch | i)) plan->append_ok = false;
+        }
+
+    // Work items.  A tile of columns sees [0, end) of the context.
+    const uint32_t tc = tile_columns(lim.shape.D), per = tc / kRowColumns;
+    const auto wide = [&](const KvSeq& q) {
+        return (uint64_t)G * q.fresh > kRowsMostColumns && lim.tiles;
+    };
+    uint64_t work[2] = {0, 0};
+    for (const KvSeq& q : plan->seqs) {
+        if (!q.fresh) continue;
+        const bool w = wide(q);
+        const uint32_t columns = w ? tc : kRowColumns;
+        const uint64_t n = ceil_div((uint64_t)G * q.fresh, columns);
+        for (uint64_t t = 0; t < n; ++t) work[w] += (uint64_t)H * tile_end(q, G, columns, (uint32_t)t);
+    }
+    const Split split[2] = {
+        {kRowColumns, kRowsStep, kRowsFewest, kRowsTarget, 2 * kRowsTarget / H + 2},
+        {tc, kTilesStep, kTilesFewest, kTilesTarget, 2 * kTilesTarget / H + 2}};
+    plan->slots = 0;
+    for (int w = 0; w < 2; ++w) {
+        const Split& sp = split[w];
+        std::vector<KvPart>& items = w ? plan->tiles : plan->rows;
+        const uint32_t first_slot = plan->slots;
+        const size_t first_join = plan->joins.size();
+        for (uint64_t most = part_tokens(work[w], sp);; most *= 2) {
+            items.clear();
+            plan->joins.resize(first_join);
+            uint32_t used = 0;  // parts with slots
+            for (uint32_t s = 0; s < num_seqs; ++s) {
+                const KvSeq& q = plan->seqs[s];
+                if (!q.fresh || wide(q) != (w == 1)) continue;
+                const uint64_t all = (uint64_t)G * q.fresh;
+                const uint32_t n = (uint32_t)ceil_div(all, sp.columns);
+                for (uint32_t t = 0; t < n; ++t) {
+                    const uint32_t end = tile_end(q, G, sp.columns, t);
+                    const uint32_t tokens_of = (uint32_t)(
+                        ceil_div(ceil_div(end, ceil_div(end, most)), sp.step) * sp.step);
+                    const uint32_t parts = (uint32_t)ceil_div(end, tokens_of);
+                    const uint32_t sub = w ? per : 1;
+                    for (uint32_t k = 0; k < parts; ++k)
+                        items.push_back({s, t, k * tokens_of, std::min(end, (k + 1) * tokens_of),
+                                         parts == 1 ? kNoSlot : first_slot + (used + k) * sub,
+                                         {}});
+                    if (parts == 1) continue;
+                    for (uint32_t c = 0; c < sub; ++c) {
+                        const uint64_t tile16 = (uint64_t)t * sub + c;
+                        if (tile16 * kRowColumns >= all) break;
+                        plan->joins.push_back(
+                            {s, (uint32_t)tile16, first_slot + used * sub + c, parts, sub, {}});
+                    }
+                    used += parts;
+                }
+            }
+            if (used <= sp.most_slots) {
+                plan->slots += used * (w ? per : 1);
+                break;
+            }
+        }
+        // Longest first, so that the last to start are the shortest.
+        std::stable_sort(items.begin(), items.end(), [](const KvPart& a, const KvPart& b) {
+            return a.end - a.begin > b.end - b.begin;
+        });
+    }
+    plan->head = {};
+    plan->head.rows = (uint32_t)plan->rows.size();
+    plan->head.tiles = (uint32_t)plan->tiles.size();
+    plan->head.joins = (uint32_t)plan->joins.size();
+    plan->head.tokens = (uint32_t)plan->tokens.size();
+    plan->head.seqs = num_seqs;
+    plan->head.append_tokens = plan->append_ok ? plan->head.tokens : 0;
+    return AQUA_OK;
+}
+
+}  // namespace aqua

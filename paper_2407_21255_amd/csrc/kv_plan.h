@@ -1,0 +1,107 @@
+// kv_plan.h -- host planning of the operators on the pool (aqua_kv_batch_set):
+// validation of a step and its split into work items.  Pure C++17, no HIP
+// types, so that it builds and is tested on a machine without a GPU.
+#pragma once
+
+#include <cstdint>
+#include <vector>
+
+#include "aqua_core.h"
+
+namespace aqua {
+
+// A column is one (new token, query head) pair of a KV head: column c of
+// sequence s is token c / G, head c % G of the G query heads that share the KV
+// head.  Two kernels share the attention by the columns that a (sequence, KV
+// head) has:
+//   rows   16 columns a workgroup, whose four waves split the tokens: bound by
+//          reading the cache;
+//   tiles  many columns a workgroup, whose waves split the columns and share
+//          the tokens through LDS: bound by the matrix products.
+// Both take parts of a context where a whole one would leave compute units
+// without work; the parts' sums are joined by a third kernel.
+constexpr uint32_t kRowColumns = 16;
+
+// Columns of a tiles workgroup, by head size: 8 waves of 32, or 4 where a
+// wave's sums take twice the registers.
+constexpr uint32_t tile_columns(uint32_t head_dim) { return head_dim > 128 ? 128 : 256; }
+
+// Up to this many columns go to the rows kernel.
+constexpr uint32_t kRowsMostColumns = 64;
+
+// Work that a launch aims at, in workgroups over all KV heads, and the fewest
+// tokens of a part (a multiple of the tokens that a workgroup takes in a step).
+constexpr uint32_t kRowsTarget = 1024;
+constexpr uint32_t kRowsStep = 128;
+constexpr uint32_t kRowsFewest = 256;
+constexpr uint32_t kTilesTarget = 512;
+constexpr uint32_t kTilesStep = 64;
+constexpr uint32_t kTilesFewest = 1024;
+
+constexpr uint32_t kMostContext = 1u << 30;
+constexpr uint32_t kNoSlot = 0xffffffffu;
+
+// Device structures, shared with the kernels.
+struct KvHeader {
+    uint32_t rows, tiles, joins, tokens, seqs;
+    uint32_t append_tokens;  // tokens that an append writes: none where it must not
+    uint32_t reserved[2];
+};
+struct alignas(16) KvSeq {
+    uint32_t first;  // of its table entries
+    uint32_t context;
+    uint32_t fresh;  // new tokens
+    uint32_t row;    // of the first of them
+};
+struct alignas(8) KvToken {
+    uint32_t block, position;
+};
+// One workgroup's work, for each KV head: the columns of tile `tile` (of 16, or
+// of tile_columns) over the tokens [begin, end).  slot: where the part's sums go
+// in the workspace, in groups of H slots; kNoSlot: the part is the whole.
+struct alignas(16) KvPart {
+    uint32_t seq, tile, begin, end, slot, reserved[3];
+};
+// One join of 16 columns, for each KV head: `parts` slots from `slot` on, one
+// every `stride` groups.
+struct alignas(16) KvJoin {
+    uint32_t seq, tile, slot, parts, stride, reserved[3];
+};
+static_assert(sizeof(KvHeader) == 32 && sizeof(KvSeq) == 16 && sizeof(KvToken) == 8 &&
+                  sizeof(KvPart) == 32 && sizeof(KvJoin) == 32,
+              "shared with the kernels");
+
+// What a batch can hold at most.
+struct KvLimits {
+    Shape shape;
+    uint32_t q_heads = 0, seqs = 0, tokens = 0, blocks = 0;
+    uint32_t group = 0;                         // G
+    uint32_t rows = 0, tiles = 0, joins = 0;    // work items
+    uint32_t slots = 0;                         // groups of H slots of 16 columns
+};
+
+// Fills *out; AQUA_ERR_INVALID for a pool or limits that the operators do not take.
+aqua_status kv_limits(const Shape& s, const aqua_kv_batch_desc* d, KvLimits* out);
+
+// A step as planned.  Keeps its memory from one to the next.
+struct KvPlan {
+    KvHeader head{};
+    std::vector<KvSeq> seqs;
+    std::vector<KvPart> rows, tiles;
+    std::vector<KvJoin> joins;
+    std::vector<KvToken> tokens;
+    uint32_t entries = 0;        // table entries
+    uint32_t longest = 0;        // context with new tokens
+    uint32_t slots = 0;          // groups used
+    bool append_ok = true;       // no written block is in another table
+    std::vector<uint64_t> mark;  // scratch: per block, (epoch, table entry)
+    uint32_t epoch = 0;
+};
+
+// Validates the step and plans it; *plan is untouched unless it returns AQUA_OK.
+// Precedence: invalid -> capacity -> range.
+aqua_status kv_plan(const KvLimits& lim, uint32_t num_seqs, const int32_t* ids,
+                    const uint64_t* offs, const uint32_t* context, const uint32_t* fresh,
+                    KvPlan* plan);
+
+}  // namespace aqua

@@ -1,0 +1,210 @@
+"""CPU tests of the operators' host planning: what a batch refuses, and that its
+work items cover every (column, token) once and stay within the batch's limits."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from tests import core_lib
+
+OK, INVALID, RANGE, CAPACITY = 0, -1, -2, -4
+F16, BF16, FP8, INT4 = 1, 2, 3, 4
+
+
+class BatchDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_uint32) for n in ("num_q_heads", "max_seqs", "max_tokens",
+                                               "max_blocks")]
+
+
+def _lib():
+    L = core_lib.lib()
+    P, u32 = ctypes.c_void_p, ctypes.c_uint32
+    L.aqua_core_kv_limits.argtypes = [P, P, P]
+    L.aqua_core_kv_plan.argtypes = [P, P, u32, P, P, P, P, u32, P, P, P, P, P]
+    L.aqua_core_kv_limits.restype = L.aqua_core_kv_plan.restype = ctypes.c_int32
+    return L
+
+
+def limits(pool, batch):
+    out = np.zeros(5, dtype=np.uint32)
+    st = _lib().aqua_core_kv_limits(ctypes.byref(core_lib.Desc(*pool)),
+                                    ctypes.byref(BatchDesc(*batch)), out.ctypes.data)
+    return st, dict(zip(("group", "rows", "tiles", "joins", "slots"), out.tolist()))
+
+
+def plan(pool, batch, tables, ctx, new, offs=None, most=1 << 16):
+    ids = np.ascontiguousarray(np.concatenate([np.asarray(t, dtype=np.int32) for t in tables])
+                               if tables else np.zeros(0, np.int32))
+    if offs is None:
+        offs = np.concatenate([[0], np.cumsum([len(t) for t in tables])])
+    offs = np.ascontiguousarray(offs, dtype=np.uint64)
+    ctx, new = (np.ascontiguousarray(x, dtype=np.uint32) for x in (ctx, new))
+    counts = np.zeros(7, dtype=np.uint32)
+    rows, tiles, joins = (np.zeros((most, 5), dtype=np.uint32) for _ in range(3))
+    tokens = np.zeros((most, 2), dtype=np.uint32)
+    st = _lib().aqua_core_kv_plan(
+        ctypes.byref(core_lib.Desc(*pool)), ctypes.byref(BatchDesc(*batch)), len(tables),
+        ids.ctypes.data, offs.ctypes.data, ctx.ctypes.data, new.ctypes.data, most,
+        *(a.ctypes.data for a in (counts, rows, tiles, joins, tokens)))
+    if st:
+        return st, None
+    c = dict(zip(("rows", "tiles", "joins", "tokens", "append_ok", "longest", "slots"),
+                 counts.tolist()))
+    return st, {"counts": c, "rows": rows[:c["rows"]], "tiles": tiles[:c["tiles"]],
+                "joins": joins[:c["joins"]], "tokens": tokens[:c["tokens"]]}
+
+
+def _tables(ctx, T, N, rng, spare=0):
+    free = rng.permutation(N)
+    out, at = [], 0
+    for c in ctx:
+        n = -(-c // T) + spare
+        out.append(free[at:at + n])
+        at += n
+    return out
+
+
+def _check_cover(pool, batch, ctx, new, p, lim):
+    """Every column's tokens once, in parts whose slots are apart and joined."""
+    L, N, H, T, D, dtype = pool
+    G = batch[0] // H
+    c = p["counts"]
+    assert c["rows"] <= lim["rows"] and c["tiles"] <= lim["tiles"]
+    assert c["joins"] <= lim["joins"] and c["slots"] <= lim["slots"]
+    wide = 128 if D > 128 else 256
+    used = {}                       # slot group -> (seq, 16-column tile)
+    parts = {}                      # (seq, columns, tile) -> [(begin, end, slot)]
+    for items, columns in ((p["rows"], 16), (p["tiles"], wide)):
+        for s, tile, begin, end, slot in items.tolist():
+            assert begin < end and begin % (128 if columns == 16 else 64) == 0
+            parts.setdefault((s, columns, tile), []).append((begin, end, slot))
+            if slot != 0xFFFFFFFF:
+                for k in range(columns // 16):
+                    assert slot + k < lim["slots"]
+                    assert slot + k not in used, "two parts in one slot"
+                    used[slot + k] = (s, tile * (columns // 16) + k, begin)
+    joins = {(s, t): (slot, n, stride) for s, t, slot, n, stride in p["joins"].tolist()}
+    assert len(joins) == len(p["joins"])
+    seen = set()
+    for (s, columns, tile), items in parts.items():
+        R = G * new[s]
+        first, last = tile * columns, min((tile + 1) * columns, R) - 1
+        assert first <= last
+        seen |= {(s, k) for k in range(first, last + 1)}
+        items.sort()
+        end = ctx[s] - new[s] + last // G + 1
+        assert items[0][0] == 0 and items[-1][1] == end
+        assert all(a[1] == b[0] for a, b in zip(items, items[1:]))
+        if len(items) == 1:
+            assert items[0][2] == 0xFFFFFFFF
+            continue
+        for k in range(columns // 16):
+            tile16 = tile * (columns // 16) + k
+            if tile16 * 16 >= R:
+                assert (s, tile16) not in joins
+                continue
+            slot, n, stride = joins.pop((s, tile16))
+            assert n == len(items)
+            assert sorted(slot + i * stride for i in range(n)) == \
+                sorted(it[2] + k for it in items)
+    assert not joins
+    assert seen == {(s, k) for s in range(len(ctx)) for k in range(G * new[s])}
+
+
+@pytest.mark.parametrize("heads", [(8, 32), (1, 71), (5, 5), (40, 40), (2, 64)])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_items_cover_every_column_once(heads, D):
+    H, Hq = heads
+    rng = np.random.default_rng(H * 1000 + D)
+    for trial in range(25):
+        T = int(rng.choice([4, 8, 16, 64]))
+        n = int(rng.integers(1, 40))
+        ctx = [int(x) for x in np.exp(rng.uniform(0, np.log(40000 if trial % 3 else 300), n))]
+        kind = trial % 4
+        new = [1 if kind == 0 else int(rng.integers(0, min(c, 7) + 1)) if kind == 1
+               else c if kind == 2 and c < 3000 else int(rng.integers(0, min(c, 700) + 1))
+               for c in ctx]
+        tables = _tables(ctx, T, sum(-(-c // T) for c in ctx) + n, rng, spare=trial % 2)
+        pool = (2, sum(len(t) for t in tables) + n, H, T, D, BF16)
+        batch = (Hq, n, max(1, sum(new)), sum(len(t) for t in tables))
+        st, lim = limits(pool, batch)
+        assert st == OK
+        st, p = plan(pool, batch, tables, ctx, new)
+        assert st == OK and p["counts"]["append_ok"] == 1
+        assert p["counts"]["longest"] == max([c for c, m in zip(ctx, new) if m], default=0)
+        _check_cover(pool, batch, ctx, new, p, lim)
+        want = [(int(t[q // T]), q) for t, c, m in zip(tables, ctx, new) for q in range(c - m, c)]
+        assert [tuple(x) for x in p["tokens"].tolist()] == want
+
+
+def test_long_contexts_are_split_and_short_ones_are_not():
+    pool, batch = (1, 9000, 8, 16, 128, BF16), (32, 64, 64, 9000)
+    rng = np.random.default_rng(2)
+    st, p = plan(pool, batch, _tables([131072], 16, 9000, rng), [131072], [1])
+    assert st == OK and 64 <= p["counts"]["rows"] <= 260
+    st, p = plan(pool, batch, _tables([200] * 64, 16, 9000, rng), [200] * 64, [1] * 64)
+    assert st == OK and p["counts"]["rows"] == 64 and p["counts"]["joins"] == 0
+    st, p = plan(pool, batch, [], [], [])
+    assert st == OK and p["counts"]["rows"] == p["counts"]["tokens"] == 0
+
+
+def test_blocks_that_two_tables_hold():
+    pool, batch = (1, 100, 2, 16, 128, BF16), (4, 4, 200, 100)
+    a, b = list(range(0, 8)), list(range(10, 18))
+    ok = lambda t, c, n: plan(pool, batch, t, c, n)[1]["counts"]["append_ok"]
+    assert ok([a, b], [100, 100], [1, 1]) == 1
+    assert ok([a, a[:6] + b[6:]], [100, 100], [1, 1]) == 1      # shared full blocks
+    assert ok([a, a], [100, 100], [1, 1]) == 0                  # both write block 6
+    assert ok([a, a], [100, 97], [1, 0]) == 0                   # one writes, one reads it
+    assert ok([a, a], [97, 96], [1, 0]) == 1                    # 96 tokens end before it
+    assert ok([a, a], [100, 100], [0, 0]) == 1                  # both read
+    assert ok([a, a], [100, 100], [20, 0]) == 0                 # writes reach block 5
+    assert ok([a[:6] + [0], b], [100, 100], [1, 1]) == 0        # a block twice in a table
+    assert ok([a + [6], b], [100, 100], [1, 1]) == 1            # entries past the context
+    assert ok([a, b[:3] + [5, 6]], [100, 48], [1, 1]) == 1      # ... of another table
+
+
+def test_what_a_batch_refuses():
+    ok = (1, 64, 2, 16, 128, BF16)
+    assert limits(ok, (4, 1, 1, 1))[0] == OK
+    for pool in [(1, 64, 2, 2, 128, BF16), (1, 64, 2, 2048, 128, BF16), (1, 64, 2, 12, 128, BF16),
+                 (1, 64, 2, 16, 96, BF16), (1, 64, 2, 16, 32, BF16), (1, 64, 2, 16, 512, BF16)]:
+        assert limits(pool, (4, 1, 1, 1))[0] == INVALID, pool
+    for batch in [(3, 1, 1, 1), (0, 1, 1, 1), (4, 0, 1, 1), (4, 1, 0, 1), (4, 1, 1, 0),
+                  (65538, 1, 1, 1), (4, (1 << 24) + 1, 1, 1), (4, 1, (1 << 28) + 1, 1)]:
+        assert limits(ok, batch)[0] == INVALID, batch
+
+
+def test_what_a_step_refuses():
+    pool, batch = (1, 64, 2, 16, 128, BF16), (4, 2, 40, 10)
+    t = [[1, 2, 3, 4], [5, 6]]
+    cases = [
+        (CAPACITY, [[1], [2], [3]], [1, 1, 1], [1, 1, 1], None),    # sequences
+        (CAPACITY, t, [64, 32], [20, 21], None),                    # tokens
+        (CAPACITY, [list(range(11))], [1], [1], None),              # table entries
+        (CAPACITY, t, [65, 32], [1, 1], None),                      # context past its table
+        (CAPACITY, [[], [1]], [1, 1], [1, 1], None),                # an empty table
+        (INVALID, t, [64, 32], [1, 33], None),                      # more new than context
+        (INVALID, t, [(1 << 30) + 1, 32], [1, 1], None),
+        (INVALID, t, [64, 32], [1, 1], [0, 4, 3]),                  # offsets
+        (INVALID, t, [64, 32], [1, 1], [1, 4, 6]),
+        (RANGE, [[1, 2, 3, 64], [5, 6]], [64, 32], [1, 1], None),
+        (RANGE, [[1, 2, 3, -1], [5, 6]], [64, 32], [1, 1], None),
+        (RANGE, [[1, 2, 3, 64], [5, 6]], [10, 32], [1, 1], None),   # unused, and still wrong
+    ]
+    for want, tables, ctx, new, offs in cases:
+        assert plan(pool, batch, tables, ctx, new, offs)[0] == want, (tables, ctx, new)
+    assert plan(pool, batch, t, [64, 32], [20, 20])[0] == OK
+    assert plan(pool, batch, [[], [1]], [0, 1], [0, 1])[0] == OK
+
+
+def test_four_bit_chunks():
+    """A 4-bit chunk is 5 bits a value; its head size is made of groups of 32."""
+    v = lambda desc, nbytes: core_lib.lib().aqua_core_validate(
+        ctypes.byref(core_lib.Desc(*desc)), 1, np.zeros(1, np.int32).ctypes.data,
+        np.array([0, 1], np.uint64).ctypes.data, 4096, nbytes, None, 0)
+    assert v((1, 4, 8, 16, 128, INT4), 20480) == OK            # 2*8*16*128 * 5/8
+    assert v((1, 4, 8, 16, 128, INT4), 20479) == CAPACITY
+    assert v((2, 4, 2, 4, 64, INT4), 2 * 640) == OK
+    for desc in [(1, 4, 8, 16, 80, INT4), (1, 4, 8, 16, 16, INT4), (1, 4, 1, 1, 32, INT4)]:
+        assert v(desc, 1 << 20) == INVALID, desc
