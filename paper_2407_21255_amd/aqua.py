@@ -710,6 +710,7 @@ class KVBatch:
         self.handle = h
         self.pool = pool
         self.num_q_heads = num_q_heads
+        self.head_dim = pool.desc.head_dim
         self.max_tokens = max_tokens
         self.tokens = 0
         pool._spaces.append(self)
@@ -729,21 +730,25 @@ class KVBatch:
             raise AquaError(st, "aqua_kv_batch_set")
         self.tokens = int(fresh.sum())
 
-    def _rows(self, t: torch.Tensor, heads: int, what: str) -> int:
+    def _needed(self, stream) -> int:
+        """Rows that a call's tensors have: the step's, or, for a call that is being
+        captured, as many as a step can ever have."""
+        if stream is None:
+            capturing = torch.cuda.is_current_stream_capturing()
+        else:
+            s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+            with torch.cuda.stream(s):
+                capturing = torch.cuda.is_current_stream_capturing()
+        return self.max_tokens if capturing else self.tokens
+
+    def _stride(self, t: torch.Tensor, heads: int, rows: int, what: str) -> int:
         """The row stride of a tensor that a call may name, after the checks that need
         its shape (the library sees an address)."""
-        D = self.pool.desc.head_dim
-        capturing = t.is_cuda and torch.cuda.is_current_stream_capturing()
-        rows = self.max_tokens if capturing else self.tokens
-        if (t.dim() != 3 or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != D
-                or not t.is_cuda or (t.numel() and (t.stride(2) != 1 or
-                                                    (heads > 1 and t.stride(1) != D)))):
+        n, s, D = t.shape, t.stride(), self.head_dim
+        if (len(n) != 3 or n[0] < rows or n[1] != heads or n[2] != D or s[2] != 1
+                or (heads > 1 and s[1] != D) or not t.is_cuda):
             raise AquaError(AQUA_ERR_INVALID, what)
-        # (A single row's stride says nothing.)
-        return t.stride(0) if t.shape[0] > 1 else heads * D
-
-    def _empty(self, q: torch.Tensor) -> torch.Tensor:
-        return torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        return s[0] if n[0] > 1 else heads * D     # (a single row's stride says nothing)
 
     @staticmethod
     def _used(stream, *tensors) -> None:
@@ -768,17 +773,19 @@ class KVBatch:
         dtype = _DTYPES.get(k.dtype)
         if dtype is None or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
             raise AquaError(AQUA_ERR_INVALID, name)
-        a = aqua_kv_append_args(k=k.data_ptr(), v=v.data_ptr(), k_stride=self._rows(k, H, name),
-                                v_stride=self._rows(v, H, name), dtype=dtype,
+        rows = self._needed(stream)
+        a = aqua_kv_append_args(k=k.data_ptr(), v=v.data_ptr(),
+                                k_stride=self._stride(k, H, rows, name),
+                                v_stride=self._stride(v, H, rows, name), dtype=dtype,
                                 interleaved=int(bool(interleaved)), k_scale=k_scale,
                                 v_scale=v_scale)
         if q is not None:
-            a.q_stride = self._rows(q, self.num_q_heads, name)
+            a.q_stride = self._stride(q, self.num_q_heads, rows, name)
             if q_out is None:
-                q_out = self._empty(q)
+                q_out = q.new_empty(q.shape)
             if q_out.dtype != q.dtype:
                 raise AquaError(AQUA_ERR_INVALID, name)
-            a.q_out_stride = self._rows(q_out, self.num_q_heads, name)
+            a.q_out_stride = self._stride(q_out, self.num_q_heads, rows, name)
             a.q, a.q_out = q.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
             raise AquaError(AQUA_ERR_INVALID, name)
@@ -803,23 +810,24 @@ class KVBatch:
         dtype = _DTYPES.get(q.dtype)
         if dtype is None:
             raise AquaError(AQUA_ERR_INVALID, name)
-        stride = self._rows(q, self.num_q_heads, name)
+        rows = self._needed(stream)
+        stride = self._stride(q, self.num_q_heads, rows, name)
         if out is None:
-            out = self._empty(q)
+            out = q.new_empty(q.shape)
         if out.dtype != q.dtype:
             raise AquaError(AQUA_ERR_INVALID, name)
         if lse is True:
-            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+            lse = q.new_empty(q.shape[:2], dtype=torch.float32)
         elif lse is False:
             lse = None
         if lse is not None and (lse.dtype != torch.float32 or lse.dim() != 2
-                                or lse.shape[0] < self.tokens
+                                or lse.shape[0] < rows
                                 or lse.shape[1] != self.num_q_heads or not lse.is_contiguous()):
             raise AquaError(AQUA_ERR_INVALID, name)
         a = aqua_kv_attend_args(
             q=q.data_ptr(), out=out.data_ptr(), lse=None if lse is None else lse.data_ptr(),
-            q_stride=stride, out_stride=self._rows(out, self.num_q_heads, name), dtype=dtype,
-            scale=self.pool.desc.head_dim ** -0.5 if scale is None else scale,
+            q_stride=stride, out_stride=self._stride(out, self.num_q_heads, rows, name), dtype=dtype,
+            scale=self.head_dim ** -0.5 if scale is None else scale,
             k_scale=k_scale, v_scale=v_scale)
         st = aqua_kv_attend(self.handle, layer, a, _stream_handle(stream))
         if st != AQUA_OK:

@@ -43,7 +43,7 @@ struct OnDevice {
 
 // Where the tables lie in the device memory and in each staging slot.
 struct Layout {
-    uint64_t seqs, rows, tiles, joins, tokens, blocks, bytes;
+    uint64_t rows, tiles, joins, tokens, blocks, bytes;
 };
 
 Layout layout_of(const aqua::KvLimits& m) {
@@ -54,7 +54,6 @@ Layout layout_of(const aqua::KvLimits& m) {
         at += (n + kAlign - 1) / kAlign * kAlign;
         return here;
     };
-    l.seqs = take(m.seqs * sizeof(aqua::KvSeq));
     l.rows = take(m.rows * sizeof(aqua::KvPart));
     l.tiles = take(m.tiles * sizeof(aqua::KvPart));
     l.joins = take(m.joins * sizeof(aqua::KvJoin));
@@ -128,7 +127,6 @@ struct aqua_kv_batch {
 
     aqua::KvTables tables() const {
         return {reinterpret_cast<const aqua::KvHeader*>(device),
-                reinterpret_cast<const aqua::KvSeq*>(device + layout.seqs),
                 reinterpret_cast<const aqua::KvPart*>(device + layout.rows),
                 reinterpret_cast<const aqua::KvPart*>(device + layout.tiles),
                 reinterpret_cast<const aqua::KvJoin*>(device + layout.joins),
@@ -142,7 +140,7 @@ struct aqua_kv_batch {
     }
     aqua::KvCounts counts(bool captured) const {
         if (captured) return {limits.rows, limits.tiles, limits.joins, limits.tokens};
-        return {plan.head.rows, plan.head.tiles, plan.head.joins, plan.head.tokens};
+        return {plan.head.rows, plan.head.tiles, plan.head.joins, plan.new_tokens};
     }
     bool takes(int32_t dtype) const {
         if (dtype != AQUA_F16 && dtype != AQUA_BF16) return false;
@@ -274,7 +272,6 @@ aqua_status aqua_kv_batch_set(aqua_kv_batch_t b, uint32_t num_seqs, const int32_
                               (uint32_t)((bytes + 15) / 16)};
     };
     piece(0, &p.head, sizeof(p.head));
-    piece(b->layout.seqs, p.seqs.data(), p.seqs.size() * sizeof(aqua::KvSeq));
     piece(b->layout.rows, p.rows.data(), p.rows.size() * sizeof(aqua::KvPart));
     piece(b->layout.tiles, p.tiles.data(), p.tiles.size() * sizeof(aqua::KvPart));
     piece(b->layout.joins, p.joins.data(), p.joins.size() * sizeof(aqua::KvJoin));
@@ -303,7 +300,7 @@ aqua_status aqua_kv_append(aqua_kv_batch_t b, uint32_t layer, const aqua_kv_appe
     OnDevice on(b->pool.device);
     if (!on.ok) return AQUA_ERR_HIP;
     const bool captured = capturing(st);
-    const uint32_t rows = captured ? b->limits.tokens : b->plan.head.tokens;
+    const uint32_t rows = captured ? b->limits.tokens : b->plan.new_tokens;
     const uint32_t q_heads = x->q ? b->limits.q_heads : 0;
     const int dev = b->pool.device;
     if (!tensor_ok(dev, x->k, rows, s.H, s.D, x->k_stride) ||
@@ -358,7 +355,7 @@ aqua_status aqua_kv_attend(aqua_kv_batch_t b, uint32_t layer, const aqua_kv_atte
     OnDevice on(b->pool.device);
     if (!on.ok) return AQUA_ERR_HIP;
     const bool captured = capturing(st);
-    const uint32_t rows = captured ? b->limits.tokens : b->plan.head.tokens;
+    const uint32_t rows = captured ? b->limits.tokens : b->plan.new_tokens;
     const uint32_t heads = b->limits.q_heads;
     const int dev = b->pool.device;
     if (!tensor_ok(dev, x->q, rows, heads, s.D, x->q_stride) ||

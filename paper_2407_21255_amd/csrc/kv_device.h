@@ -93,11 +93,21 @@ __device__ inline uint32_t pair_hi(uint32_t a, uint32_t b) {
 template <int I>
 __device__ inline f16x2 codes4(uint32_t w) {
     const uint32_t s = I == 0 ? w << 6 : I == 1 ? w << 2 : I == 2 ? w >> 2 : w >> 6;
-    return __builtin_bit_cast(f16x2, (s & 0x03c003c0u) | 0x4c004c00u);
+    // (Constants in registers: two in one and-or, and not an and and an or.)
+    uint32_t mask = 0x03c003c0u, sixteen = 0x4c004c00u;
+    asm("" : "+s"(mask));
+    asm("" : "+s"(sixteen));
+    return __builtin_bit_cast(f16x2, (s & mask) | sixteen);
 }
 // The two values that they stand for: one rounding, as the format has it.
 __device__ inline uint32_t value4(f16x2 c, f16x2 scale, f16x2 base) {
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(c, scale, base));
+}
+
+// A load of data that is read once.
+template <typename T>
+__device__ inline T once(const void* p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const T*>(p));
 }
 
 __device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -186,6 +196,18 @@ __device__ inline void fit_queries(typename Mat<M>::v8 (&qf)[N], float* scale2, 
         }
         *scale2 = __builtin_amdgcn_ldexpf(*scale2, -e);
     }
+}
+
+// Makes the scores' scale positive: queries change their sign with it, so that the
+// largest product is the largest score.  A scale of 0 becomes the least there is, with
+// which all scores are 0 and masked ones, -inf, stay what they are.
+template <typename V8, int N>
+__device__ inline void fit_scale(V8 (&qf)[N], float* scale2) {
+    if (*scale2 < 0.0f)
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            qf[n] = __builtin_bit_cast(V8, __builtin_bit_cast(u32x4, qf[n]) ^ 0x80008000u);
+    *scale2 = fmaxf(fabsf(*scale2), 1.17549435e-38f);
 }
 
 // The softmax is computed in powers of two.  The running maximum is raised only when

@@ -13,7 +13,6 @@ namespace aqua {
 // A batch's tables in device memory, as aqua_kv_batch_set left them.
 struct KvTables {
     const KvHeader* head;
-    const KvSeq* seqs;
     const KvPart* rows;
     const KvPart* tiles;
     const KvJoin* joins;
@@ -76,7 +75,7 @@ constexpr uint64_t slot_floats(uint32_t head_dim) { return kRowColumns * (head_d
 
 // Copies pieces of pinned memory to device memory with one launch.
 struct KvUpload {
-    static constexpr uint32_t kPieces = 7;
+    static constexpr uint32_t kPieces = 6;
     struct {
         const uint4* src;
         uint4* dst;

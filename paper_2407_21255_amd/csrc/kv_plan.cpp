@@ -10,15 +10,48 @@ namespace {
 
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
-struct Split {
-    uint32_t columns, step, fewest, target, most_slots;
-};
+// An item to split: its tokens.
+uint64_t parts_of(const std::vector<uint32_t>& ends, uint64_t most) {
+    uint64_t n = 0;
+    for (uint32_t e : ends) n += ceil_div(e, most);
+    return n;
+}
 
-// Tokens of a part so that all items of a kernel together make about `target`
-// workgroups.
-uint64_t part_tokens(uint64_t work, const Split& sp) {
-    const uint64_t n = ceil_div(ceil_div(work, sp.target), sp.step) * sp.step;
-    return std::max<uint64_t>(n, sp.fewest);
+// Tokens of a part at most.  Workgroups start longest first, so a launch of r rounds
+// of `wide` ends after r parts of the longest size, or the work of all spread evenly
+// and one part more, whichever is less; every round starts its parts anew.  For each
+// number of rounds the smallest parts that fit them are found by bisection, and
+// the rounds that end first are taken.
+uint64_t part_tokens(const std::vector<uint32_t>& ends, uint32_t H, const KvSplit& sp) {
+    uint64_t work = 0, longest = 0;
+    for (uint32_t e : ends) {
+        work += (uint64_t)H * e;
+        longest = std::max<uint64_t>(longest, e);
+    }
+    if (longest <= sp.fewest) return sp.fewest;
+    const uint64_t whole = ceil_div(longest, sp.step) * sp.step, even = ceil_div(work, sp.wide);
+    const auto cost = [&](uint64_t rounds, uint64_t most) {
+        return std::min(rounds * most, even + most) + rounds * sp.start;
+    };
+    uint64_t best = whole, least = cost(ceil_div(ends.size() * (uint64_t)H, sp.wide), whole);
+    for (uint64_t r = 1; r <= sp.rounds; ++r) {
+        const uint64_t fit = r * sp.wide;
+        if (ends.size() * (uint64_t)H > fit) continue;
+        uint64_t lo = sp.fewest / sp.step, hi = whole / sp.step;  // hi fits
+        while (lo < hi) {
+            const uint64_t mid = (lo + hi) / 2;
+            if (parts_of(ends, mid * sp.step) * H <= fit)
+                hi = mid;
+            else
+                lo = mid + 1;
+        }
+        const uint64_t c = cost(r, hi * sp.step);
+        if (c < least) {
+            least = c;
+            best = hi * sp.step;
+        }
+    }
+    return best;
 }
 
 // Tokens that the columns of a tile see at most.
@@ -47,8 +80,8 @@ aqua_status kv_limits(const Shape& s, const aqua_kv_batch_desc* d, KvLimits* out
     m.blocks = d->max_blocks;
     m.group = m.q_heads / s.H;
     const uint64_t G = m.group, H = s.H;
-    // Items of whole contexts: a sequence's columns round up to a tile.  Items
-    // that splitting adds: at most `target` workgroups.
+    // Items of whole contexts: a sequence's columns round up to a tile.  Splitting makes
+    // at most wide * rounds workgroups of the items that it is used for.
     const uint64_t busy = std::min(m.seqs, m.tokens);
     const uint64_t wide = std::min<uint64_t>(busy, G * m.tokens / (kRowsMostColumns + 1));
     const uint32_t tc = tile_columns(s.D);
@@ -57,15 +90,16 @@ aqua_status kv_limits(const Shape& s, const aqua_kv_batch_desc* d, KvLimits* out
     // (A single token's heads may be more columns than kRowsMostColumns; they go to
     // the tiles kernel, whose items are fewer.)
     const uint64_t tiles = wide ? wide + G * m.tokens / tc : 0;
-    // Slots: a split item has at least two parts of half a part's tokens each,
-    // so splitting makes at most twice the target.
-    const uint64_t row_slots = 2 * kRowsTarget / H + 2;
-    const uint64_t tile_slots = tiles ? (2 * kTilesTarget / H + 2) * (tc / kRowColumns) : 0;
-    const uint64_t most_rows = rows + 2 * kRowsTarget / H + 2;
-    const uint64_t most_tiles = tiles ? tiles + 2 * kTilesTarget / H + 2 : 0;
-    const uint64_t joins = (row_slots + tile_slots) / 2;
+    const uint64_t row_slots = kRows.wide * kRows.rounds / H;
+    const uint64_t tile_slots = tiles ? kTiles.wide * kTiles.rounds / H * (tc / kRowColumns) : 0;
+    const uint64_t most_rows = std::max(rows, row_slots);
+    const uint64_t most_tiles = tiles ? std::max<uint64_t>(tiles, kTiles.wide * kTiles.rounds / H) : 0;
+    // A tile of 16 with p >= 2 parts makes at most 1 + 16 turns / groups joins, with
+    // turns <= p / kJoinAhead + 1 (and groups / turns rounded down: twice that).
+    const uint64_t joins =
+        (row_slots + tile_slots) * (kRowColumns + join_groups(s.D)) / join_groups(s.D) + 16;
     if (most_rows * H > 0x7fffffffull || most_tiles * H > 0x7fffffffull ||
-        joins * H * 4 > 0x7fffffffull || (row_slots + tile_slots) * H > 0x7fffffffull)
+        joins * H > 0x7fffffffull || (row_slots + tile_slots) * H > 0x7fffffffull)
         return AQUA_ERR_INVALID;
     m.rows = (uint32_t)most_rows;
     m.tiles = (uint32_t)most_tiles;
@@ -139,55 +173,49 @@ aqua_status kv_plan(const KvLimits& lim, uint32_t num_seqs, const int32_t* ids,
     const auto wide = [&](const KvSeq& q) {
         return (uint64_t)G * q.fresh > kRowsMostColumns && lim.tiles;
     };
-    uint64_t work[2] = {0, 0};
-    for (const KvSeq& q : plan->seqs) {
-        if (!q.fresh) continue;
-        const bool w = wide(q);
-        const uint32_t columns = w ? tc : kRowColumns;
-        const uint64_t n = ceil_div((uint64_t)G * q.fresh, columns);
-        for (uint64_t t = 0; t < n; ++t) work[w] += (uint64_t)H * tile_end(q, G, columns, (uint32_t)t);
-    }
-    const Split split[2] = {
-        {kRowColumns, kRowsStep, kRowsFewest, kRowsTarget, 2 * kRowsTarget / H + 2},
-        {tc, kTilesStep, kTilesFewest, kTilesTarget, 2 * kTilesTarget / H + 2}};
     plan->slots = 0;
     for (int w = 0; w < 2; ++w) {
-        const Split& sp = split[w];
+        const KvSplit& sp = w ? kTiles : kRows;
+        const uint32_t columns = w ? tc : kRowColumns, sub = w ? per : 1;
         std::vector<KvPart>& items = w ? plan->tiles : plan->rows;
-        const uint32_t first_slot = plan->slots;
-        const size_t first_join = plan->joins.size();
-        for (uint64_t most = part_tokens(work[w], sp);; most *= 2) {
-            items.clear();
-            plan->joins.resize(first_join);
-            uint32_t used = 0;  // parts with slots
-            for (uint32_t s = 0; s < num_seqs; ++s) {
-                const KvSeq& q = plan->seqs[s];
-                if (!q.fresh || wide(q) != (w == 1)) continue;
-                const uint64_t all = (uint64_t)G * q.fresh;
-                const uint32_t n = (uint32_t)ceil_div(all, sp.columns);
-                for (uint32_t t = 0; t < n; ++t) {
-                    const uint32_t end = tile_end(q, G, sp.columns, t);
-                    const uint32_t tokens_of = (uint32_t)(
-                        ceil_div(ceil_div(end, ceil_div(end, most)), sp.step) * sp.step);
-                    const uint32_t parts = (uint32_t)ceil_div(end, tokens_of);
-                    const uint32_t sub = w ? per : 1;
-                    for (uint32_t k = 0; k < parts; ++k)
-                        items.push_back({s, t, k * tokens_of, std::min(end, (k + 1) * tokens_of),
-                                         parts == 1 ? kNoSlot : first_slot + (used + k) * sub,
-                                         {}});
-                    if (parts == 1) continue;
-                    for (uint32_t c = 0; c < sub; ++c) {
-                        const uint64_t tile16 = (uint64_t)t * sub + c;
-                        if (tile16 * kRowColumns >= all) break;
-                        plan->joins.push_back(
-                            {s, (uint32_t)tile16, first_slot + used * sub + c, parts, sub, {}});
-                    }
-                    used += parts;
+        plan->ends.clear();
+        for (const KvSeq& q : plan->seqs)
+            if (q.fresh && wide(q) == (w == 1))
+                for (uint64_t t = 0; t * columns < (uint64_t)G * q.fresh; ++t)
+                    plan->ends.push_back(tile_end(q, G, columns, (uint32_t)t));
+        if (plan->ends.empty()) continue;
+        const uint64_t most = part_tokens(plan->ends, H, sp);
+        for (const KvSeq& q : plan->seqs) {
+            if (!q.fresh || wide(q) != (w == 1)) continue;
+            const uint64_t all = (uint64_t)G * q.fresh;
+            for (uint32_t t = 0; (uint64_t)t * columns < all; ++t) {
+                const uint32_t end = tile_end(q, G, columns, t);
+                const uint32_t n = (uint32_t)ceil_div(end, most);
+                if (n == 1) {
+                    items.push_back({q, t, 0, end, kNoSlot});
+                    continue;
                 }
-            }
-            if (used <= sp.most_slots) {
-                plan->slots += used * (w ? per : 1);
-                break;
+                // Parts of one size, in whole steps: n of them or fewer.
+                const uint32_t size = (uint32_t)(ceil_div(ceil_div(end, n), sp.step) * sp.step);
+                const uint32_t parts = (uint32_t)ceil_div(end, size);
+                for (uint32_t k = 0; k < parts; ++k)
+                    items.push_back({q, t, k * size, std::min(end, (k + 1) * size),
+                                     plan->slots + k * sub});
+                const uint32_t groups = join_groups(lim.shape.D);
+                const uint32_t turns =
+                    std::min<uint32_t>(groups, (uint32_t)ceil_div(parts, kJoinAhead));
+                const uint32_t take = std::min(groups / turns, kRowColumns);
+                const uint32_t last =
+                    (uint32_t)std::min<uint64_t>((uint64_t)(t + 1) * columns, all);
+                for (uint32_t c = t * columns; c < last;) {
+                    const uint32_t room = kRowColumns - c % kRowColumns;
+                    const uint32_t n16 = std::min({take, room, last - c});
+                    plan->joins.push_back({q.row, c, n16,
+                                           plan->slots + (c - t * columns) / kRowColumns, parts,
+                                           sub, {}});
+                    c += n16;
+                }
+                plan->slots += parts * sub;
             }
         }
         // Longest first, so that the last to start are the shortest.
@@ -199,9 +227,8 @@ aqua_status kv_plan(const KvLimits& lim, uint32_t num_seqs, const int32_t* ids,
     plan->head.rows = (uint32_t)plan->rows.size();
     plan->head.tiles = (uint32_t)plan->tiles.size();
     plan->head.joins = (uint32_t)plan->joins.size();
-    plan->head.tokens = (uint32_t)plan->tokens.size();
-    plan->head.seqs = num_seqs;
-    plan->head.append_tokens = plan->append_ok ? plan->head.tokens : 0;
+    plan->new_tokens = (uint32_t)plan->tokens.size();
+    plan->head.append_tokens = plan->append_ok ? plan->new_tokens : 0;
     return AQUA_OK;
 }
 

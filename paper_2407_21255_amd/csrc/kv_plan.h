@@ -29,25 +29,27 @@ constexpr uint32_t tile_columns(uint32_t head_dim) { return head_dim > 128 ? 128
 // Up to this many columns go to the rows kernel.
 constexpr uint32_t kRowsMostColumns = 64;
 
-// Work that a launch aims at, in workgroups over all KV heads, and the fewest
-// tokens of a part (a multiple of the tokens that a workgroup takes in a step).
-constexpr uint32_t kRowsTarget = 1024;
-constexpr uint32_t kRowsStep = 128;
-constexpr uint32_t kRowsFewest = 256;
-constexpr uint32_t kTilesTarget = 512;
-constexpr uint32_t kTilesStep = 64;
-constexpr uint32_t kTilesFewest = 1024;
+// How a kernel's items are split into parts of at most `most` tokens (part_tokens):
+//   wide     workgroups that run at once;
+//   step     tokens that a workgroup takes in a step: parts are whole ones;
+//   fewest   tokens of a part that is worth a join (see kRows, kTiles);
+//   rounds   workgroups are at most `wide` times this, but for those of whole items;
+//   start    what starting a part costs, in tokens.
+struct KvSplit {
+    uint32_t wide, step, fewest, rounds, start;
+};
+constexpr KvSplit kRows{512, 256, 512, 8, 64};
+constexpr KvSplit kTiles{256, 64, 512, 4, 128};
 
 constexpr uint32_t kMostContext = 1u << 30;
 constexpr uint32_t kNoSlot = 0xffffffffu;
 
 // Device structures, shared with the kernels.
 struct KvHeader {
-    uint32_t rows, tiles, joins, tokens, seqs;
+    uint32_t rows, tiles, joins;
     uint32_t append_tokens;  // tokens that an append writes: none where it must not
-    uint32_t reserved[2];
 };
-struct alignas(16) KvSeq {
+struct KvSeq {
     uint32_t first;  // of its table entries
     uint32_t context;
     uint32_t fresh;  // new tokens
@@ -57,18 +59,25 @@ struct alignas(8) KvToken {
     uint32_t block, position;
 };
 // One workgroup's work, for each KV head: the columns of tile `tile` (of 16, or
-// of tile_columns) over the tokens [begin, end).  slot: where the part's sums go
-// in the workspace, in groups of H slots; kNoSlot: the part is the whole.
+// of tile_columns) of a sequence over the tokens [begin, end).  slot: where the part's
+// sums go in the workspace, in groups of H slots; kNoSlot: the part is the whole.
+// It holds all that its workgroup has to know, so that one load brings it.
 struct alignas(16) KvPart {
-    uint32_t seq, tile, begin, end, slot, reserved[3];
+    KvSeq seq;
+    uint32_t tile, begin, end, slot;
 };
-// One join of 16 columns, for each KV head: `parts` slots from `slot` on, one
-// every `stride` groups.
+// One workgroup's join, for each KV head: `count` columns from `column` on (of the
+// sequence's), all of one tile of 16, whose sums are in `parts` slots from `slot` on,
+// one every `stride` groups.
 struct alignas(16) KvJoin {
-    uint32_t seq, tile, slot, parts, stride, reserved[3];
+    uint32_t row, column, count, slot, parts, stride, reserved[2];
 };
-static_assert(sizeof(KvHeader) == 32 && sizeof(KvSeq) == 16 && sizeof(KvToken) == 8 &&
-                  sizeof(KvPart) == 32 && sizeof(KvJoin) == 32,
+// A joining workgroup has this many groups of lanes, each with four values of a column
+// a lane, and takes so many columns that a group has about kJoinAhead parts.
+constexpr uint32_t join_groups(uint32_t head_dim) { return 1024 / head_dim; }
+constexpr uint32_t kJoinAhead = 8;
+static_assert(sizeof(KvHeader) == 16 && sizeof(KvToken) == 8 && sizeof(KvPart) == 32 &&
+                  sizeof(KvJoin) == 32,
               "shared with the kernels");
 
 // What a batch can hold at most.
@@ -91,9 +100,11 @@ struct KvPlan {
     std::vector<KvJoin> joins;
     std::vector<KvToken> tokens;
     uint32_t entries = 0;        // table entries
+    uint32_t new_tokens = 0;
     uint32_t longest = 0;        // context with new tokens
     uint32_t slots = 0;          // groups used
     bool append_ok = true;       // no written block is in another table
+    std::vector<uint32_t> ends;  // scratch: tokens of a kernel's items
     std::vector<uint64_t> mark;  // scratch: per block, (epoch, table entry)
     uint32_t epoch = 0;
 };

@@ -3,18 +3,22 @@
 // of the split sums.
 //
 // One pass over the tokens with a running maximum and sum.  Bound by reading the
-// cache: each key and value byte is read once, straight from the pool's blocks into
-// the registers that the matrix instructions take, with no LDS in between:
+// cache, each key and value byte once:
 //   S^T = K Q^T   16x16x32: A = keys (a lane holds one token's 8 values), B =
 //                 queries, so a lane's scores are of one column (lane % 16) and
-//                 of tokens 4 (lane / 16) + 0..3 of each 16;
+//                 of four tokens of each 16;
 //   O^T += V^T P^T  A = values, B = weights.  The order of the tokens inside a product
 //                 is free, so the lane's eight scores of 32 tokens are its B operand
-//                 as they stand, and the values are loaded in that order: lane
-//                 group kg takes tokens 4 kg + 0..3 and 16 + 4 kg + 0..3.  A lane
-//                 loads D/16 consecutive values of its 8 tokens, and pairing their
-//                 halves gives the operands of D/16 products.
-// All statistics and sums are fp32.
+//                 as they stand, and the values are taken in that order.  A lane takes
+//                 D/16 consecutive values of its 8 tokens, and pairing their halves
+//                 gives the operands of D/16 products.
+// Pools of 16 bits are loaded straight into the registers that the products take
+// (Direct).  In 8 and 4 bits a lane's share of a value row would be 8 or 4 bytes, and
+// there a wave loads whole pieces of 16 bytes a lane and exchanges them through LDS
+// that is its own (Staged).  Either way the next step is on its way while one is
+// computed.  All statistics and sums are fp32.
+#include <algorithm>
+
 #include "kv_device.h"
 
 namespace aqua {
@@ -22,10 +26,9 @@ namespace {
 
 using namespace kv;
 
-constexpr int kWaves = 4, kStep = 32;  // tokens of a wave's step
-static_assert(kRowsStep == kWaves * kStep, "parts are whole steps of a workgroup");
+constexpr int kWaves = 4;
 
-// Keys of a 16-token tile as a lane loads them, and the values of a 32-token step.
+// Keys of a 16-token tile as a lane holds them, and the values of 32 tokens.
 // first_of(ks, kg): first of the 8 values of a head that lane group kg puts into
 // product ks.
 template <int POOL, int D>
@@ -40,19 +43,19 @@ struct Load16 {
     __device__ static void key(Key& k, const uint8_t* row, const uint8_t*, int kg) {
 #pragma unroll
         for (int i = 0; i < kK; ++i)
-            k.w[i] = *reinterpret_cast<const u32x4*>(row + i * 64 + kg * 16);
+            k.w[i] = once<u32x4>(row + i * 64 + kg * 16);
     }
     template <typename M>
     __device__ static u32x4 key_of(const Key& k, int ks) { return k.w[ks]; }
     __device__ static void val(Val& v, int i, const uint8_t* row, const uint8_t*, int m) {
         if constexpr (kV == 2) {
-            const u32x2 w = *reinterpret_cast<const u32x2*>(row + m * 8);
+            const u32x2 w = once<u32x2>(row + m * 8);
             v.w[i][0] = w[0];
             v.w[i][1] = w[1];
         } else {
 #pragma unroll
             for (int j = 0; j < kV; j += 4) {
-                const u32x4 w = *reinterpret_cast<const u32x4*>(row + m * (4 * kV) + 4 * j);
+                const u32x4 w = once<u32x4>(row + m * (4 * kV) + 4 * j);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v.w[i][j + e] = w[e];
             }
@@ -212,22 +215,178 @@ struct Load<kInt4, D> {
     }
 };
 
+// Where a head's keys and values are, and a sequence's blocks.
+struct Cache {
+    const uint8_t *keys, *vals, *kpairs, *vpairs;  // of block 0
+    uint64_t chunk;
+    const int32_t* table;
+    uint32_t last, shift, mask;  // table entries are read up to `last`; slots
+    // (A step may reach behind the context: the last block is read there instead.)
+    __device__ uint32_t block(uint32_t token) const { return table[min(token >> shift, last)]; }
+};
+
+// Keys and values that are loaded as the products take them: a lane's token of keys is
+// lane % 16 of each 16, and lane group kg takes the values of tokens 4 kg + 0..3.
+template <int POOL, int D>
+struct Direct {
+    using L = Load<POOL, D>;
+    static constexpr int kStep = 32;
+    static constexpr bool kStaged = false;
+    static constexpr uint32_t kRow = row_bytes<POOL>(D), kBytes = 0;
+    typename L::Key keys[2];
+    typename L::Val vals;
+    uint32_t kb[2], vb[2];
+    __device__ static int token(int kg, int r) { return 4 * kg + r; }
+    __device__ void blocks(const Cache& c, uint32_t t, int lane) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            kb[i] = c.block(t + 16 * i + lane % 16);
+            vb[i] = c.block(t + 16 * i + 4 * (lane / 16));
+        }
+    }
+    __device__ void fetch_keys(const Cache& c, uint32_t t, int lane) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            L::key(keys[i],
+                   c.keys + kb[i] * c.chunk + ((t + 16 * i + lane % 16) & c.mask) * kRow, nullptr,
+                   lane / 16);
+    }
+    __device__ void fetch_vals(const Cache& c, uint32_t t, int lane) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint8_t* r =
+                c.vals + vb[i] * c.chunk + ((t + 16 * i + 4 * (lane / 16)) & c.mask) * kRow;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) L::val(vals, 4 * i + j, r + j * kRow, nullptr, lane % 16);
+        }
+    }
+    __device__ void settle(uint8_t*, int) {}
+    __device__ typename L::Key key(const uint8_t*, int i, int) const { return keys[i]; }
+    __device__ typename L::Val val(const uint8_t*, int, int) const { return vals; }
+};
+
+// Keys and values that pass through LDS: pieces of 16 bytes in the rows' order.
+// Product row m of 16 is token 4 (m % 4) + m / 4, so that lane group kg takes the
+// values of tokens 4 r + kg: the four groups' reads are of four rows that follow each
+// other, and fall on different banks.
+template <int POOL, int D, int STEP>
+struct Staged {
+    using L = Load<POOL, D>;
+    static constexpr int kStep = STEP;
+    static constexpr bool kStaged = true;
+    static constexpr uint32_t kRow = row_bytes<POOL>(D), kPairs = POOL == kInt4 ? D / 32 * 4 : 0;
+    static constexpr int kPieces = STEP * kRow / 1024;             // a lane's, of keys
+    static constexpr uint32_t kPair = STEP * kPairs < 1024 ? 8 : 16;  // bytes of a piece of pairs
+    static constexpr int kPairPieces = STEP * kPairs / (64 * kPair);
+    static_assert(kPieces * 1024 == STEP * kRow && kPairPieces * 64 * kPair == STEP * kPairs,
+                  "whole pieces");
+    static constexpr uint32_t kRowPairs = kPairs ? kPairs / kPair : 1;  // pieces of a row
+    static constexpr uint32_t kKeyAt = 0, kValAt = STEP * kRow, kKeyPairAt = 2 * STEP * kRow,
+                              kValPairAt = kKeyPairAt + STEP * kPairs,
+                              kBytes = kValPairAt + STEP * kPairs;
+    u32x4 k[kPieces], v[kPieces], kp[kPairPieces + 1], vp[kPairPieces + 1];
+    uint32_t b[kPieces], pb[kPairPieces + 1];
+    __device__ static int token(int kg, int r) { return 4 * r + kg; }
+    __device__ static uint32_t row_of(int j, int lane) { return (j * 64 + lane) / (kRow / 16); }
+    __device__ static uint32_t pair_row_of(int j, int lane) {
+        return (j * 64 + lane) / kRowPairs;
+    }
+    __device__ void blocks(const Cache& c, uint32_t t, int lane) {
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) b[j] = c.block(t + row_of(j, lane));
+#pragma unroll
+        for (int j = 0; j < kPairPieces; ++j) pb[j] = c.block(t + pair_row_of(j, lane));
+    }
+    __device__ void fetch_keys(const Cache& c, uint32_t t, int lane) {
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+            const uint64_t at = b[j] * c.chunk + ((t + row_of(j, lane)) & c.mask) * kRow +
+                                (j * 64 + lane) % (kRow / 16) * 16;
+            k[j] = once<u32x4>(c.keys + at);
+            v[j] = once<u32x4>(c.vals + at);
+        }
+#pragma unroll
+        for (int j = 0; j < kPairPieces; ++j) {
+            const uint64_t at = pb[j] * c.chunk + ((t + pair_row_of(j, lane)) & c.mask) * kPairs +
+                                (j * 64 + lane) % kRowPairs * kPair;
+            if constexpr (kPair == 16) {
+                kp[j] = once<u32x4>(c.kpairs + at);
+                vp[j] = once<u32x4>(c.vpairs + at);
+            } else {
+                const u32x2 x = once<u32x2>(c.kpairs + at), y = once<u32x2>(c.vpairs + at);
+                kp[j] = u32x4{x[0], x[1], 0, 0};
+                vp[j] = u32x4{y[0], y[1], 0, 0};
+            }
+        }
+    }
+    __device__ void fetch_vals(const Cache&, uint32_t, int) {}
+    __device__ void settle(uint8_t* lds, int lane) {
+        // A wave's LDS instructions are done in their order; the fences keep the compiler
+        // from changing it.
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+            *reinterpret_cast<u32x4*>(lds + kKeyAt + (j * 64 + lane) * 16) = k[j];
+            *reinterpret_cast<u32x4*>(lds + kValAt + (j * 64 + lane) * 16) = v[j];
+        }
+#pragma unroll
+        for (int j = 0; j < kPairPieces; ++j) {
+            uint8_t* const x = lds + kKeyPairAt + (j * 64 + lane) * kPair;
+            uint8_t* const y = lds + kValPairAt + (j * 64 + lane) * kPair;
+            if constexpr (kPair == 16) {
+                *reinterpret_cast<u32x4*>(x) = kp[j];
+                *reinterpret_cast<u32x4*>(y) = vp[j];
+            } else {
+                *reinterpret_cast<u32x2*>(x) = u32x2{kp[j][0], kp[j][1]};
+                *reinterpret_cast<u32x2*>(y) = u32x2{vp[j][0], vp[j][1]};
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    }
+    __device__ typename L::Key key(const uint8_t* lds, int i, int lane) const {
+        const uint32_t row = 16 * i + lane % 4 * 4 + lane % 16 / 4;
+        typename L::Key x;
+        L::key(x, lds + kKeyAt + row * kRow, lds + kKeyPairAt + row * kPairs, lane / 16);
+        return x;
+    }
+    __device__ typename L::Val val(const uint8_t* lds, int half, int lane) const {
+        typename L::Val x;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t row = 32 * half + i / 4 * 16 + token(lane / 16, i % 4);
+            L::val(x, i, lds + kValAt + row * kRow, lds + kValPairAt + row * kPairs, lane % 16);
+        }
+        return x;
+    }
+};
+
+template <int POOL, int D>
+struct Source : Direct<POOL, D> {};
+template <int D>
+struct Source<kFP8, D> : Staged<kFP8, D, 32> {};
+template <int D>
+struct Source<kInt4, D> : Staged<kInt4, D, D == 64 ? 64 : 32> {};   // whole pieces a wave
+
 // Q: type of the queries and the result.  M: type of the products: fp16 for a 4-bit
 // pool, whose values are fp16 numbers.
+// Two waves a SIMD at least, where their registers allow it (heads up to 128).
 template <int POOL, typename Q, int D>
-__global__ __launch_bounds__(256) void rows_kernel(const KvAttend a) {
+__global__ __launch_bounds__(256, D > 128 ? 1 : 2) void rows_kernel(const KvAttend a) {
     using M = std::conditional_t<POOL == kInt4, f16, Q>;
     using L = Load<POOL, D>;
+    using S = Source<POOL, D>;
     using V8 = typename Mat<M>::v8;
-    constexpr int E = L::E;
+    constexpr int E = L::E, kStep = S::kStep, kTiles = kStep / 16;
+    constexpr bool kTwo = std::is_same_v<M, Q>;
+    static_assert(kRows.step % (kWaves * kStep) == 0, "parts are whole steps of a workgroup");
     const uint32_t H = a.layer.H;
     const uint32_t item = blockIdx.x / H, head = blockIdx.x % H;
+    const KvPart part = a.t.rows[item];   // (an old one, where there is none)
     if (item >= a.t.head->rows) return;
-    const KvPart part = a.t.rows[item];
-    const KvSeq seq = a.t.seqs[part.seq];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const KvSeq seq = part.seq;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int col = lane % 16, kg = lane / 16;
-    const uint32_t G = a.group, T = a.layer.T, shift = a.layer.shift;
+    const uint32_t G = a.group, T = a.layer.T;
     const uint32_t columns = G * seq.fresh;
     const uint32_t c = min(part.tile * kRowColumns + col, columns - 1);
     const uint32_t token = c / G;
@@ -245,86 +404,75 @@ __global__ __launch_bounds__(256) void rows_kernel(const KvAttend a) {
         qf[ks] = __builtin_bit_cast(
             V8, *reinterpret_cast<const u32x4*>(q + 2 * L::first_of(ks, kg)));
     fit_queries<M, Q>(qf, &scale2, [](float x) { return over_rows(x, Max()); });
+    fit_scale(qf, &scale2);
 
     constexpr uint32_t kRow = row_bytes<POOL>(D), kPairs = D / 32 * 4;
-    const uint64_t C = a.layer.chunk_bytes;
-    const uint8_t* const kbase = a.layer.base + (uint64_t)head * T * kRow;
-    const uint8_t* const vbase = kbase + (uint64_t)H * T * kRow;
-    const uint8_t* const kpair = a.layer.base + (uint64_t)2 * H * T * kRow + (uint64_t)head * T * kPairs;
-    const uint8_t* const vpair = kpair + (uint64_t)H * T * kPairs;
-    const int32_t* const table = a.t.blocks + seq.first;
-    const uint32_t last = (seq.context - 1) >> shift;   // table entries are read up to here
+    Cache cache;
+    cache.keys = a.layer.base + (uint64_t)head * T * kRow;
+    cache.vals = cache.keys + (uint64_t)H * T * kRow;
+    cache.kpairs = a.layer.base + (uint64_t)2 * H * T * kRow + (uint64_t)head * T * kPairs;
+    cache.vpairs = cache.kpairs + (uint64_t)H * T * kPairs;
+    cache.chunk = a.layer.chunk_bytes;
+    cache.table = a.t.blocks + seq.first;
+    cache.last = (seq.context - 1) >> a.layer.shift;
+    cache.shift = a.layer.shift;
+    cache.mask = T - 1;
+
+    // Steps of the waves, then the waves' sums.
+    constexpr uint32_t kSumRow = D + 4;
+    __shared__ __attribute__((aligned(16)))
+    uint8_t shared[std::max<uint32_t>(kWaves * S::kBytes, kWaves * 16 * kSumRow * 4)];
+    uint8_t* const lds = shared + wave * S::kBytes;
 
     f32x4 acc[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = f32x4{0, 0, 0, 0};
     float top = -__builtin_inff(), sum = 0.0f;
     bool odd = false;
-
-    typename L::Key key[2];
-    typename L::Val val;
-    uint32_t kb[2], vb[2];
-    // Blocks of the lane's tokens in the step at t: two keys, two runs of 4 values.
-    // A step may reach behind the context: the last block is read there instead.
-    const auto blocks = [&](uint32_t t) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            kb[i] = table[min((t + 16 * i + col) >> shift, last)];
-            vb[i] = table[min((t + 16 * i + 4 * kg) >> shift, last)];
-        }
-    };
-    const auto load_keys = [&](uint32_t t) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t slot = (t + 16 * i + col) & (T - 1);
-            L::key(key[i], kbase + kb[i] * C + slot * kRow, kpair + kb[i] * C + slot * kPairs, kg);
-        }
-    };
-    const auto load_vals = [&](uint32_t t) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t slot = (t + 16 * i + 4 * kg) & (T - 1);
-            const uint8_t* r = vbase + vb[i] * C + slot * kRow;
-            const uint8_t* p = vpair + vb[i] * C + slot * kPairs;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) L::val(val, 4 * i + j, r + j * kRow, p + j * kPairs, col);
-        }
-    };
+    S src;
 
     uint32_t t = part.begin + wave * kStep;
     if (t < part.end) {
-        blocks(t);
-        load_keys(t);
-        load_vals(t);
-        blocks(t + kWaves * kStep);
+        src.blocks(cache, t, lane);
+        src.fetch_keys(cache, t, lane);
+        src.fetch_vals(cache, t, lane);
+        src.blocks(cache, t + kWaves * kStep, lane);
     }
     for (; t < part.end; t += kWaves * kStep) {
-        f32x4 s[2];
+        const uint32_t next = t + kWaves * kStep;
+        const bool more = next < part.end;
+        src.settle(lds, lane);
+        if (S::kStaged && more) {
+            src.fetch_keys(cache, next, lane);
+            src.blocks(cache, next + kWaves * kStep, lane);
+        }
+        f32x4 s[kTiles];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kTiles; ++i) {
             s[i] = f32x4{0, 0, 0, 0};
+            const typename L::Key key = src.key(lds, i, lane);
 #pragma unroll
             for (int ks = 0; ks < D / 32; ++ks)
                 s[i] = Mat<M>::mfma16(
-                    __builtin_bit_cast(V8, L::template key_of<M>(key[i], ks)), qf[ks], s[i]);
+                    __builtin_bit_cast(V8, L::template key_of<M>(key, ks)), qf[ks], s[i]);
         }
-        const uint32_t next = t + kWaves * kStep;
-        const bool more = next < part.end;
-        if (more) load_keys(next);
+        if (!S::kStaged && more) src.fetch_keys(cache, next, lane);
 
         // Tokens behind a column's limit, or another part's, get no weight.
         const uint32_t stop = min(limit, part.end);
         const bool masked = t + kStep > min(least, part.end);
+        if (masked)
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (t + 16 * i + S::token(kg, r) >= stop) s[i][r] = -__builtin_inff();
         float high = -__builtin_inff();
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                s[i][r] *= scale2;
-                if (masked && t + 16 * i + 4 * kg + r >= stop) s[i][r] = -__builtin_inff();
-                high = fmaxf(high, s[i][r]);
-            }
-        high = over_rows(high, Max());
+            for (int r = 0; r < 4; ++r) high = fmaxf(high, s[i][r]);
+        high = over_rows(high, Max()) * scale2;
         if (__any(high > top + kSlack)) {
             // (A column that has seen nothing keeps its -inf, and sums of 0.)
             const float raised = fmaxf(top, high);
@@ -335,42 +483,51 @@ __global__ __launch_bounds__(256) void rows_kernel(const KvAttend a) {
             for (int e = 0; e < E; ++e) acc[e] *= f;
         }
         const float off = top > -__builtin_inff() ? top - kLift : 0.0f;
-        u32x4 pw;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            float p[4];
+        for (int half = 0; half < kTiles / 2; ++half) {
+            // Where the products' type is no finer than the result's, weights are in two
+            // terms, the second what the first's rounding left: the products have time to
+            // spare, and the result is as exact as its own rounding.
+            u32x4 pw, pr = {0, 0, 0, 0};
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                p[r] = exp2_(s[i][r] - off);
-                sum += p[r];
+            for (int i = 0; i < 4; ++i) {
+                const float x = exp2_(__builtin_fmaf(s[2 * half + i / 2][i % 2 * 2], scale2, -off));
+                const float y =
+                    exp2_(__builtin_fmaf(s[2 * half + i / 2][i % 2 * 2 + 1], scale2, -off));
+                sum += x + y;
+                const uint32_t w = pack2<M>(x, y);
+                pw[i] = w;
+                if (kTwo) pr[i] = pack2<M>(x - lo_float<M>(w), y - hi_float<M>(w));
             }
-            pw[2 * i] = pack2<M>(p[0], p[1]);
-            pw[2 * i + 1] = pack2<M>(p[2], p[3]);
-        }
-        const V8 pf = __builtin_bit_cast(V8, pw);
+            const V8 pf = __builtin_bit_cast(V8, pw), pg = __builtin_bit_cast(V8, pr);
 
-        u32x4 vf[E];
-        if (masked) {
-            // What stands behind the context may be anything: no weight is no help
-            // against NaN.
+            typename L::Val val = src.val(lds, half, lane);
+            if (masked) {
+                // What stands behind the context may be anything: no weight is no help
+                // against NaN.
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < 8; ++i)
+                    if (t + 32 * half + i / 4 * 16 + S::token(kg, i % 4) >= seq.context)
+                        L::clear(val, i);
+            }
+            u32x4 vf[E];
+            L::template vals_of<M>(val, vf);
+            if (masked && seq.fresh > 1)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (t + 16 * i + 4 * kg + j >= seq.context) L::clear(val, 4 * i + j);
-        }
-        L::template vals_of<M>(val, vf);
-        if (masked && seq.fresh > 1)
+                for (int e = 0; e < E; ++e)
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) vf[e][p] = finite_or_zero<M>(vf[e][p], &odd);
 #pragma unroll
             for (int e = 0; e < E; ++e)
+                acc[e] = Mat<M>::mfma16(__builtin_bit_cast(V8, vf[e]), pf, acc[e]);
+            if (kTwo)
 #pragma unroll
-                for (int p = 0; p < 4; ++p) vf[e][p] = finite_or_zero<M>(vf[e][p], &odd);
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            acc[e] = Mat<M>::mfma16(__builtin_bit_cast(V8, vf[e]), pf, acc[e]);
-        if (more) {
-            load_vals(next);
-            blocks(next + kWaves * kStep);
+                for (int e = 0; e < E; ++e)
+                    acc[e] = Mat<M>::mfma16(__builtin_bit_cast(V8, vf[e]), pg, acc[e]);
+        }
+        if (!S::kStaged && more) {
+            src.fetch_vals(cache, next, lane);
+            src.blocks(cache, next + kWaves * kStep, lane);
         }
     }
 
@@ -378,14 +535,14 @@ __global__ __launch_bounds__(256) void rows_kernel(const KvAttend a) {
         for (t = part.begin + wave * kStep; t < part.end; t += kWaves * kStep) {
             if (t + kStep <= min(least, part.end)) continue;
             for (uint32_t k = t; k < min(t + kStep, part.end); ++k) {
-                const uint64_t at = table[k >> shift] * C;
-                const uint32_t slot = k & (T - 1);
+                const uint64_t at = cache.block(k) * cache.chunk;
+                const uint32_t slot = k & cache.mask;
 #pragma unroll
                 for (int e = 0; e < E; ++e)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const float x = odd_value<POOL, M>(vbase + at + slot * kRow,
-                                                           vpair + at + slot * kPairs,
+                        const float x = odd_value<POOL, M>(cache.vals + at + slot * kRow,
+                                                           cache.vpairs + at + slot * kPairs,
                                                            (kg * 4 + r) * E + e);
                         acc[e][r] += k < min(limit, part.end) ? x : 0.0f;
                     }
@@ -394,10 +551,10 @@ __global__ __launch_bounds__(256) void rows_kernel(const KvAttend a) {
 
     // The waves' sums, on a common maximum.
     __shared__ float tops[kWaves][16], sums[kWaves][16];
-    __shared__ __attribute__((aligned(16))) float part_sum[kWaves][16][D + 4];
+    float (*part_sum)[16][kSumRow] = reinterpret_cast<float (*)[16][kSumRow]>(shared);
     sum = over_rows(sum, Sum());
     if (kg == 0) tops[wave][col] = top;
-    __syncthreads();
+    __syncthreads();   // and the waves are done with their steps
     float all = tops[0][col];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) all = fmaxf(all, tops[w][col]);
@@ -462,51 +619,98 @@ __global__ __launch_bounds__(256) void rows_kernel(const KvAttend a) {
         a.lse[row * a.q_heads + h] = (high - kLift + __builtin_log2f(total)) * kLn2;
 }
 
-// Joins the parts of 16 columns: a wave a column, four columns a workgroup.
-// Lanes take four values each and, where a column has fewer than 256, the parts in
-// turn.  Every sum has a fixed order.
+// A running maximum, sum of weights and weighted values.
+struct Sums {
+    float top = -__builtin_inff(), total = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
+    // Brings the sums to a maximum that is at least their own.
+    __device__ void raise(float to) {
+        // (Where nothing has been seen, -inf, the sums are 0.)
+        const float f = exp2_(top - (to > -__builtin_inff() ? to : 0.0f));
+        total *= f;
+        o *= f;
+        top = to;
+    }
+    __device__ void add(float high, float sum, f32x4 x) {
+        const float w = exp2_(high - (top > -__builtin_inff() ? top : 0.0f));
+        total += w * sum;
+        o += w * x;
+    }
+};
+
+// Parts p, p + turns, ... of a column: AHEAD of them in flight.
+template <int AHEAD>
+__device__ inline void join_parts(Sums& s, const float* first, uint64_t step, uint32_t at,
+                                  uint32_t stat, uint32_t p, uint32_t turns, uint32_t parts) {
+    for (; p < parts; p += AHEAD * turns) {
+        float high[AHEAD], sum[AHEAD], raised = s.top;
+        f32x4 x[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            // (The last turn reads the last part again, and drops it.)
+            const float* slot = first + min(p + i * turns, parts - 1) * step;
+            high[i] = slot[stat];
+            sum[i] = slot[stat + kRowColumns];
+            x[i] = *reinterpret_cast<const f32x4*>(slot + at);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) raised = fmaxf(raised, high[i]);
+        s.raise(raised);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (p + i * turns < parts) s.add(high[i], sum[i], x[i]);
+    }
+}
+
+// Joins the parts of some columns of a tile of 16.  A lane takes four values of a
+// column; the groups of lanes that the columns leave over share out the parts.  Bound by
+// latency, so each lane has up to kJoinAhead parts in flight, and there is one
+// pass with a running maximum.  Every sum has a fixed order.
 template <typename Q, int D>
 __global__ __launch_bounds__(256) void join_kernel(const KvAttend a) {
-    const uint32_t H = a.layer.H;
-    const uint32_t quarter = blockIdx.x % 4, head = blockIdx.x / 4 % H, item = blockIdx.x / 4 / H;
-    if (item >= a.t.head->joins) return;
-    const KvJoin join = a.t.joins[item];
-    const KvSeq seq = a.t.seqs[join.seq];
-    const uint32_t col = quarter * 4 + threadIdx.x / 64, c = join.tile * kRowColumns + col;
-    if (c >= a.group * seq.fresh) return;
-    const int lane = threadIdx.x % 64;
-    constexpr int kLanes = D / 4, kTurns = 64 / kLanes;
-    const uint64_t step = (uint64_t)join.stride * H * slot_floats(D);
-    const float* first = a.t.slots + ((uint64_t)join.slot * H + head) * slot_floats(D);
-
-    float top = -__builtin_inff();
-    for (uint32_t p = lane; p < join.parts; p += 64)
-        top = fmaxf(top, first[p * step + 16 * D + col]);
-#pragma unroll
-    for (int m = 32; m; m /= 2) top = fmaxf(top, __shfl_xor(top, m));
-    const int turn = lane / kLanes, d = lane % kLanes * 4;
-    f32x4 o = {0, 0, 0, 0};
-    float total = 0.0f;
-#pragma unroll 4
-    for (uint32_t p = turn; p < join.parts; p += kTurns) {
-        const float* slot = first + p * step;
-        const float w = exp2_(slot[16 * D + col] - top);
-        total += w * slot[16 * D + 16 + col];
-        o += w * *reinterpret_cast<const f32x4*>(slot + col * D + d);
+    constexpr uint32_t kLanes = D / 4, kGroups = join_groups(D);
+    static_assert(kLanes * kGroups == 256, "a workgroup's lanes");
+    __shared__ f32x4 os[kGroups][kLanes];
+    __shared__ float tops[kGroups][kLanes], totals[kGroups][kLanes];
+    const uint32_t H = a.layer.H, group = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+    const uint32_t items = a.t.head->joins * H;
+    // (A captured launch may have fewer workgroups than joins.)
+    for (uint32_t n = blockIdx.x; n < items; n += gridDim.x) {
+        const KvJoin join = a.t.joins[n / H];
+        const uint32_t head = n % H, turns = kGroups / join.count;
+        const uint32_t mine = group / turns, turn = group % turns;
+        const bool live = mine < join.count;
+        const uint32_t c = join.column + min(mine, join.count - 1), col = c % kRowColumns;
+        const uint64_t step = (uint64_t)join.stride * H * slot_floats(D);
+        const float* first = a.t.slots + ((uint64_t)join.slot * H + head) * slot_floats(D);
+        const uint32_t at = col * D + lane * 4, stat = 16 * D + col;
+        Sums s;
+        if (join.parts <= 2 * turns)
+            join_parts<2>(s, first, step, at, stat, turn, turns, join.parts);
+        else
+            join_parts<kJoinAhead>(s, first, step, at, stat, turn, turns, join.parts);
+        if (turns > 1) {
+            os[group][lane] = s.o;
+            tops[group][lane] = s.top;
+            totals[group][lane] = s.total;
+            __syncthreads();
+            if (turn == 0 && live) {
+                float top = s.top;
+                for (uint32_t t = 1; t < turns; ++t) top = fmaxf(top, tops[group + t][lane]);
+                s.raise(top);
+                for (uint32_t t = 1; t < turns; ++t)
+                    s.add(tops[group + t][lane], totals[group + t][lane], os[group + t][lane]);
+            }
+            __syncthreads();
+        }
+        if (!live || turn) continue;
+        const uint64_t row = join.row + c / a.group, h = head * a.group + c % a.group;
+        const float norm = a.v_scale / s.total;
+        *reinterpret_cast<u32x2*>(a.out + 2 * (row * a.out_stride + h * D + lane * 4)) =
+            u32x2{pack2<Q>(s.o[0] * norm, s.o[1] * norm), pack2<Q>(s.o[2] * norm, s.o[3] * norm)};
+        if (a.lse && lane == 0)
+            a.lse[row * a.q_heads + h] = (s.top - kLift + __builtin_log2f(s.total)) * kLn2;
     }
-#pragma unroll
-    for (int m = kLanes; m < 64; m *= 2) {
-        total += __shfl_xor(total, m);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], m);
-    }
-    if (turn) return;
-    const uint64_t row = seq.row + c / a.group, h = head * a.group + c % a.group;
-    const float norm = a.v_scale / total;
-    *reinterpret_cast<u32x2*>(a.out + 2 * (row * a.out_stride + h * D + d)) =
-        u32x2{pack2<Q>(o[0] * norm, o[1] * norm), pack2<Q>(o[2] * norm, o[3] * norm)};
-    if (a.lse && d == 0)
-        a.lse[row * a.q_heads + h] = (top - kLift + __builtin_log2f(total)) * kLn2;
 }
 
 template <typename K>
@@ -534,6 +738,9 @@ hipError_t join(const KvAttend& a, uint32_t grid, hipStream_t stream) {
     }
 }
 
+// Workgroups of a join's launch at most.
+constexpr uint32_t kJoinGrid = 4096;
+
 }  // namespace
 
 hipError_t launch_rows(const KvAttend& a, uint32_t items, hipStream_t stream) {
@@ -552,7 +759,7 @@ hipError_t launch_rows(const KvAttend& a, uint32_t items, hipStream_t stream) {
 
 hipError_t launch_join(const KvAttend& a, uint32_t joins, hipStream_t stream) {
     if (!joins) return hipSuccess;
-    const uint32_t grid = joins * a.layer.H * 4;
+    const uint32_t all = joins * a.layer.H, grid = all < kJoinGrid ? all : kJoinGrid;
     return a.dtype == AQUA_F16 ? join<f16>(a, grid, stream) : join<bf16>(a, grid, stream);
 }
 

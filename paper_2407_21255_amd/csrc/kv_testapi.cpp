@@ -22,9 +22,9 @@ aqua_status aqua_core_kv_limits(const aqua_kv_desc* pool, const aqua_kv_batch_de
 }
 
 // Plans a step; counts: rows, tiles, joins, tokens, append_ok, longest, slots.
-// rows, tiles: 5 words an item (seq, tile, begin, end, slot); joins: 5 words (seq,
-// tile, slot, parts, stride); tokens: 2 words (block, position); at most `most` of
-// each are written.
+// rows, tiles: 8 words an item (first, context, fresh, row, tile, begin, end, slot);
+// joins: 6 words (row, column, count, slot, parts, stride); tokens: 2 words (block,
+// position); at most `most` of each are written.
 aqua_status aqua_core_kv_plan(const aqua_kv_desc* pool, const aqua_kv_batch_desc* d,
                               uint32_t num_seqs, const int32_t* ids, const uint64_t* offs,
                               const uint32_t* context, const uint32_t* fresh, uint32_t most,
@@ -39,16 +39,16 @@ aqua_status aqua_core_kv_plan(const aqua_kv_desc* pool, const aqua_kv_batch_desc
     aqua::KvPlan p;
     st = aqua::kv_plan(m, num_seqs, ids, offs, context, fresh, &p);
     if (st != AQUA_OK) return st;
-    const uint32_t c[7] = {p.head.rows, p.head.tiles,  p.head.joins, p.head.tokens,
+    const uint32_t c[7] = {p.head.rows, p.head.tiles,  p.head.joins, p.new_tokens,
                            p.append_ok, p.longest, p.slots};
     std::memcpy(counts, c, sizeof(c));
     for (uint32_t i = 0; i < std::min<uint32_t>(most, p.head.rows); ++i)
-        std::memcpy(rows + 5 * i, &p.rows[i], 20);
+        std::memcpy(rows + 8 * i, &p.rows[i], 32);
     for (uint32_t i = 0; i < std::min<uint32_t>(most, p.head.tiles); ++i)
-        std::memcpy(tiles + 5 * i, &p.tiles[i], 20);
+        std::memcpy(tiles + 8 * i, &p.tiles[i], 32);
     for (uint32_t i = 0; i < std::min<uint32_t>(most, p.head.joins); ++i)
-        std::memcpy(joins + 5 * i, &p.joins[i], 20);
-    for (uint32_t i = 0; i < std::min<uint32_t>(most, p.head.tokens); ++i)
+        std::memcpy(joins + 6 * i, &p.joins[i], 24);
+    for (uint32_t i = 0; i < std::min<uint32_t>(most, p.new_tokens); ++i)
         std::memcpy(tokens + 2 * i, &p.tokens[i], 8);
     return AQUA_OK;
 }

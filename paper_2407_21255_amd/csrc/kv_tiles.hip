@@ -1,11 +1,11 @@
 // kv_tiles.hip -- attention for many columns (prompts and chunks of them): 256
-// columns a workgroup (128 for heads of 256), a wave 32, over tiles of 64 tokens
+// columns a workgroup (128 for heads of 256), a wave 32, over tiles of 64 tokens (32)
 // that the waves share through LDS.
 //
 // One pass over the tokens with a running maximum and sum.  Bound by the matrix
 // products and, next to them, by the exponentials of the weights.  Per tile and wave:
 //   S^T = K Q^T     32x32x16: A = keys from LDS, B = queries, which stay in
-//                   registers; a lane's 32 scores are of one column (lane % 32);
+//                   registers; a lane's scores are of one column (lane % 32);
 //   O^T += V^T P^T  A = values from LDS, B = the lane's weights as they stand: a
 //                   16-token product takes, from lane half h, tokens 4h + 0..3 and
 //                   8 + 4h + 0..3 of its 16, and V^T lies in LDS in that order.
@@ -21,8 +21,8 @@ namespace {
 
 using namespace kv;
 
-constexpr int kTile = 64;
-static_assert(kTilesStep == kTile, "parts are whole tiles");
+// Tokens of a tile: heads of 256 leave no registers for more.
+constexpr int tile_tokens(int D) { return D > 128 ? 32 : 64; }
 
 // What a thread brings of a tile: units of 16 keys' values (of one token) and of 4
 // tokens times 4 values.
@@ -136,15 +136,17 @@ struct Raw<kInt4, D> {
     }
 };
 
-// Byte offset of 16-byte piece `piece` of key row `row`, and of value row `d` (64
-// tokens of one value), in a buffer.
+// Byte offset of 16-byte piece `piece` of key row `row`, and of value row `d` (the
+// tile's tokens of one value), in a buffer.
 template <int D>
 __device__ inline uint32_t key_at(uint32_t row, uint32_t piece) {
     const uint32_t x = D == 64 ? (row >> 1) & 7 : row & 15;
     return row * (2 * D) + (piece ^ x) * 16;
 }
+template <int TILE>
 __device__ inline uint32_t val_at(uint32_t d, uint32_t piece) {
-    return d * (2 * kTile) + (piece ^ (((d >> 1) ^ (d >> 4)) & 7)) * 16;
+    const uint32_t x = TILE == 64 ? ((d >> 1) ^ (d >> 4)) & 7 : ((d >> 2) ^ (d >> 4)) & 3;
+    return d * (2 * TILE) + (piece ^ x) * 16;
 }
 
 template <int POOL, typename Q, int D>
@@ -152,14 +154,16 @@ __global__ __launch_bounds__(2 * (int)tile_columns(D)) void tiles_kernel(const K
     using M = std::conditional_t<POOL == kInt4, f16, Q>;
     using V8 = typename Mat<M>::v8;
     constexpr int kColumns = tile_columns(D), kThreads = 2 * kColumns;
-    constexpr int kUnits = 4 * D, kPer = (kUnits + kThreads - 1) / kThreads;
-    constexpr int kSteps = D / 16, kRows = D / 32;
+    constexpr int kTile = tile_tokens(D), kRuns = kTile / 16, kWide = kTile / 32;
+    static_assert(kTiles.step % kTile == 0, "parts are whole tiles");
+    constexpr int kUnits = kTile * D / 16, kPer = (kUnits + kThreads - 1) / kThreads;
+    constexpr int kSteps = D / 16, kOut = D / 32;
     const uint32_t H = a.layer.H;
     const uint32_t item = blockIdx.x / H, head = blockIdx.x % H;
+    const KvPart part = a.t.tiles[item];   // (an old one, where there is none)
     if (item >= a.t.head->tiles) return;
-    const KvPart part = a.t.tiles[item];
-    const KvSeq seq = a.t.seqs[part.seq];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const KvSeq seq = part.seq;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int col = lane % 32, half = lane / 32;
     const uint32_t G = a.group, T = a.layer.T, shift = a.layer.shift;
     const uint32_t columns = G * seq.fresh;
@@ -183,6 +187,7 @@ __global__ __launch_bounds__(2 * (int)tile_columns(D)) void tiles_kernel(const K
         qf[ks] = __builtin_bit_cast(
             V8, *reinterpret_cast<const u32x4*>(q + 2 * (ks * 16 + half * 8)));
     fit_queries<M, Q>(qf, &scale2, [](float x) { return over_halves(x, Max()); });
+    fit_scale(qf, &scale2);
 
     constexpr uint32_t kRow = row_bytes<POOL>(D), kPairs = D / 32 * 4;
     const uint64_t C = a.layer.chunk_bytes;
@@ -260,16 +265,22 @@ __global__ __launch_bounds__(2 * (int)tile_columns(D)) void tiles_kernel(const K
             const uint32_t p = quad / 4 * 2 + quad % 2, at = quad / 2 % 2 * 8;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                *reinterpret_cast<u32x2*>(&vals[buf][val_at(d4 * 4 + j, p) + at]) = vw[j];
+                *reinterpret_cast<u32x2*>(&vals[buf][val_at<kTile>(d4 * 4 + j, p) + at]) = vw[j];
         }
     };
+    // Value row 32 dt + col's piece of run kt: the exchange makes it the piece that
+    // row col has for run kt xor dt.
+    uint32_t val_pos[kRuns];
+#pragma unroll
+    for (int k = 0; k < kRuns; ++k) val_pos[k] = val_at<kTile>(col, k * 2 + half);
     const auto val_of = [&](int buf, int dt, int kt) {
-        return *reinterpret_cast<const u32x4*>(&vals[buf][val_at(dt * 32 + col, kt * 2 + half)]);
+        return *reinterpret_cast<const u32x4*>(
+            &vals[buf][val_pos[kt ^ (dt & (kRuns - 1))] + dt * 64 * kTile]);
     };
 
-    f32x16 acc[kRows];
+    f32x16 acc[kOut];
 #pragma unroll
-    for (int d = 0; d < kRows; ++d)
+    for (int d = 0; d < kOut; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[d][r] = 0.0f;
     float top = -__builtin_inff(), sum = 0.0f;
@@ -283,33 +294,37 @@ __global__ __launch_bounds__(2 * (int)tile_columns(D)) void tiles_kernel(const K
         blocks(part.begin + 2 * kTile);
     }
     __syncthreads();
-    int buf = 0;
-    for (uint32_t t = part.begin; t < part.end; t += kTile, buf ^= 1) {
+    // The tile at t, in buffer `buf`; the next goes into the other.
+    const auto tile = [&](auto buffer, uint32_t t) {
+        constexpr int buf = decltype(buffer)::value;
         if (t < most) {
-            f32x16 s[2];
+            f32x16 s[kWide];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < kWide; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[i][r] = 0.0f;
 #pragma unroll
-                for (int ks = 0; ks < kSteps; ++ks) {
+            for (int ks = 0; ks < kSteps; ++ks)
+#pragma unroll
+                for (int i = 0; i < kWide; ++i) {
                     const u32x4 k = *reinterpret_cast<const u32x4*>(
                         &keys[buf][key_at<D>(i * 32 + col, ks * 2 + half)]);
                     s[i] = Mat<M>::mfma32(__builtin_bit_cast(V8, k), qf[ks], s[i]);
                 }
+            if (t + kTile > least) {
+#pragma unroll
+                for (int i = 0; i < kWide; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (t + 32 * i + 8 * (r / 4) + 4 * half + r % 4 >= stop)
+                            s[i][r] = -__builtin_inff();
             }
-            const bool masked = t + kTile > least;
             float high = -__builtin_inff();
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < kWide; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[i][r] *= scale2;
-                    if (masked && t + 32 * i + 8 * (r / 4) + 4 * half + r % 4 >= stop)
-                        s[i][r] = -__builtin_inff();
-                    high = fmaxf(high, s[i][r]);
-                }
-            high = over_halves(high, Max());
+                for (int r = 0; r < 16; ++r) high = fmaxf(high, s[i][r]);
+            high = over_halves(high, Max()) * scale2;
             if (__any(high > top + kSlack)) {
                 // (A column that has seen nothing keeps its -inf, and sums of 0.)
                 const float raised = fmaxf(top, high);
@@ -317,28 +332,29 @@ __global__ __launch_bounds__(2 * (int)tile_columns(D)) void tiles_kernel(const K
                 top = raised;
                 sum *= f;
 #pragma unroll
-                for (int d = 0; d < kRows; ++d)
+                for (int d = 0; d < kOut; ++d)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) acc[d][r] *= f;
             }
             const float off = top > -__builtin_inff() ? top - kLift : 0.0f;
-            V8 pf[4];
+            V8 pf[kRuns];
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt) {
+            for (int kt = 0; kt < kRuns; ++kt) {
                 u32x4 w;
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
-                    const float x = exp2_(s[kt / 2][kt % 2 * 8 + 2 * p] - off);
-                    const float y = exp2_(s[kt / 2][kt % 2 * 8 + 2 * p + 1] - off);
+                    const int r = kt % 2 * 8 + 2 * p;
+                    const float x = exp2_(__builtin_fmaf(s[kt / 2][r], scale2, -off));
+                    const float y = exp2_(__builtin_fmaf(s[kt / 2][r + 1], scale2, -off));
                     sum += x + y;
                     w[p] = pack2<M>(x, y);
                 }
                 pf[kt] = __builtin_bit_cast(V8, w);
             }
 #pragma unroll
-            for (int d = 0; d < kRows; ++d)
+            for (int kt = 0; kt < kRuns; ++kt)
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
+                for (int d = 0; d < kOut; ++d)
                     acc[d] = Mat<M>::mfma32(__builtin_bit_cast(V8, val_of(buf, d, kt)), pf[kt],
                                             acc[d]);
         }
@@ -350,6 +366,10 @@ __global__ __launch_bounds__(2 * (int)tile_columns(D)) void tiles_kernel(const K
             }
         }
         __syncthreads();
+    };
+    for (uint32_t t = part.begin; t < part.end; t += 2 * kTile) {
+        tile(std::integral_constant<int, 0>(), t);
+        if (t + kTile < part.end) tile(std::integral_constant<int, 1>(), t + kTile);
     }
 
     if (odd) {
@@ -359,7 +379,7 @@ __global__ __launch_bounds__(2 * (int)tile_columns(D)) void tiles_kernel(const K
             const uint64_t at = table[k >> shift] * C;
             const uint32_t slot = k & (T - 1);
 #pragma unroll
-            for (int d = 0; d < kRows; ++d)
+            for (int d = 0; d < kOut; ++d)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const float x = odd_value<POOL, M>(vbase + at + slot * kRow,
@@ -376,7 +396,7 @@ __global__ __launch_bounds__(2 * (int)tile_columns(D)) void tiles_kernel(const K
         float* slot =
             a.t.slots + ((uint64_t)(part.slot + w / kRowColumns) * H + head) * slot_floats(D);
 #pragma unroll
-        for (int d = 0; d < kRows; ++d)
+        for (int d = 0; d < kOut; ++d)
 #pragma unroll
             for (int r = 0; r < 16; r += 4)
                 *reinterpret_cast<f32x4*>(slot + oc * D + d * 32 + r * 2 + half * 4) =
@@ -391,7 +411,7 @@ __global__ __launch_bounds__(2 * (int)tile_columns(D)) void tiles_kernel(const K
     const float norm = a.v_scale / sum;
     uint8_t* out = a.out + 2 * (row * a.out_stride + h * D);
 #pragma unroll
-    for (int d = 0; d < kRows; ++d)
+    for (int d = 0; d < kOut; ++d)
 #pragma unroll
         for (int r = 0; r < 16; r += 4)
             *reinterpret_cast<u32x2*>(out + 2 * (d * 32 + r * 2 + half * 4)) =

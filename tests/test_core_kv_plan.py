@@ -40,7 +40,7 @@ def plan(pool, batch, tables, ctx, new, offs=None, most=1 << 16):
     offs = np.ascontiguousarray(offs, dtype=np.uint64)
     ctx, new = (np.ascontiguousarray(x, dtype=np.uint32) for x in (ctx, new))
     counts = np.zeros(7, dtype=np.uint32)
-    rows, tiles, joins = (np.zeros((most, 5), dtype=np.uint32) for _ in range(3))
+    rows, tiles, joins = (np.zeros((most, n), dtype=np.uint32) for n in (8, 8, 6))
     tokens = np.zeros((most, 2), dtype=np.uint32)
     st = _lib().aqua_core_kv_plan(
         ctypes.byref(core_lib.Desc(*pool)), ctypes.byref(BatchDesc(*batch)), len(tables),
@@ -64,7 +64,7 @@ def _tables(ctx, T, N, rng, spare=0):
     return out
 
 
-def _check_cover(pool, batch, ctx, new, p, lim):
+def _check_cover(pool, batch, starts, ctx, new, p, lim):
     """Every column's tokens once, in parts whose slots are apart and joined."""
     L, N, H, T, D, dtype = pool
     G = batch[0] // H
@@ -72,19 +72,27 @@ def _check_cover(pool, batch, ctx, new, p, lim):
     assert c["rows"] <= lim["rows"] and c["tiles"] <= lim["tiles"]
     assert c["joins"] <= lim["joins"] and c["slots"] <= lim["slots"]
     wide = 128 if D > 128 else 256
+    firsts = np.concatenate([[0], np.cumsum(new)]).tolist()
+    by_row = {firsts[s]: s for s in range(len(ctx)) if new[s]}
     used = {}                       # slot group -> (seq, 16-column tile)
     parts = {}                      # (seq, columns, tile) -> [(begin, end, slot)]
     for items, columns in ((p["rows"], 16), (p["tiles"], wide)):
-        for s, tile, begin, end, slot in items.tolist():
-            assert begin < end and begin % (128 if columns == 16 else 64) == 0
+        for at, context, fresh, row, tile, begin, end, slot in items.tolist():
+            s = by_row[row]
+            assert (at, context, fresh) == (starts[s], ctx[s], new[s])
+            assert begin < end and begin % (256 if columns == 16 else 64) == 0
             parts.setdefault((s, columns, tile), []).append((begin, end, slot))
             if slot != 0xFFFFFFFF:
                 for k in range(columns // 16):
                     assert slot + k < lim["slots"]
                     assert slot + k not in used, "two parts in one slot"
                     used[slot + k] = (s, tile * (columns // 16) + k, begin)
-    joins = {(s, t): (slot, n, stride) for s, t, slot, n, stride in p["joins"].tolist()}
-    assert len(joins) == len(p["joins"])
+    joins = {}
+    for row, column, count, slot, n, stride in p["joins"].tolist():
+        assert count and column // 16 == (column + count - 1) // 16
+        for k in range(column, column + count):
+            assert (by_row[row], k) not in joins, "a column is joined twice"
+            joins[by_row[row], k] = (slot, n, stride)
     seen = set()
     for (s, columns, tile), items in parts.items():
         R = G * new[s]
@@ -100,13 +108,11 @@ def _check_cover(pool, batch, ctx, new, p, lim):
             continue
         for k in range(columns // 16):
             tile16 = tile * (columns // 16) + k
-            if tile16 * 16 >= R:
-                assert (s, tile16) not in joins
-                continue
-            slot, n, stride = joins.pop((s, tile16))
-            assert n == len(items)
-            assert sorted(slot + i * stride for i in range(n)) == \
-                sorted(it[2] + k for it in items)
+            for column in range(tile16 * 16, min((tile16 + 1) * 16, R)):
+                slot, n, stride = joins.pop((s, column))
+                assert n == len(items)
+                assert sorted(slot + i * stride for i in range(n)) == \
+                    sorted(it[2] + k for it in items)
     assert not joins
     assert seen == {(s, k) for s in range(len(ctx)) for k in range(G * new[s])}
 
@@ -132,7 +138,8 @@ def test_items_cover_every_column_once(heads, D):
         st, p = plan(pool, batch, tables, ctx, new)
         assert st == OK and p["counts"]["append_ok"] == 1
         assert p["counts"]["longest"] == max([c for c, m in zip(ctx, new) if m], default=0)
-        _check_cover(pool, batch, ctx, new, p, lim)
+        _check_cover(pool, batch, np.cumsum([0] + [len(t) for t in tables])[:-1].tolist(), ctx, new,
+                     p, lim)
         want = [(int(t[q // T]), q) for t, c, m in zip(tables, ctx, new) for q in range(c - m, c)]
         assert [tuple(x) for x in p["tokens"].tolist()] == want
 
