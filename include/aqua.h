@@ -107,7 +107,8 @@ enum {
  *         little-endian 32-bit word, e0 e2 e4 e6 are in bits 0-3, 4-7, 8-11,
  *         12-15 and e1 e3 e5 e7 in bits 16-19 ... 28-31 (so that a shift and a
  *         mask leave two neighbours in the two halves of a register);
- *   pairs [2][H][T][D/32] of {scale, base}, behind all codes of the chunk. */
+ *   pairs [2][H][T][D/32] of {scale, base}, behind all codes of the chunk.
+ *         All 16 values of a pair are finite, or scale or base is not. */
 enum { AQUA_F16 = 1, AQUA_BF16 = 2, AQUA_FP8_E4M3 = 3, AQUA_INT4 = 4 };
 
 /* Offload targets.  DEVICE: device memory on the pool's GPU (a carved-out

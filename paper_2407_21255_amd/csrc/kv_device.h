@@ -93,10 +93,11 @@ __device__ inline uint32_t pair_hi(uint32_t a, uint32_t b) {
 template <int I>
 __device__ inline f16x2 codes4(uint32_t w) {
     const uint32_t s = I == 0 ? w << 6 : I == 1 ? w << 2 : I == 2 ? w >> 2 : w >> 6;
-    // (Constants in registers: two in one and-or, and not an and and an or.)
+    // (Constants in registers, one of them a vector register: an instruction takes one
+    // scalar.  Then it is one and-or, and not an and and an or.)
     uint32_t mask = 0x03c003c0u, sixteen = 0x4c004c00u;
     asm("" : "+s"(mask));
-    asm("" : "+s"(sixteen));
+    asm("" : "+v"(sixteen));
     return __builtin_bit_cast(f16x2, (s & mask) | sixteen);
 }
 // The two values that they stand for: one rounding, as the format has it.
@@ -104,10 +105,11 @@ __device__ inline uint32_t value4(f16x2 c, f16x2 scale, f16x2 base) {
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(c, scale, base));
 }
 
-// A load of data that is read once.
-template <typename T>
-__device__ inline T once(const void* p) {
-    return __builtin_nontemporal_load(reinterpret_cast<const T*>(p));
+// A load; ONCE: of data that nothing else reads.
+template <bool ONCE, typename T>
+__device__ inline T load(const void* p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const T*>(p));
+    return *reinterpret_cast<const T*>(p);
 }
 
 __device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }

@@ -40,22 +40,24 @@ struct Load16 {
     struct Key { u32x4 w[kK]; };
     struct Val { uint32_t w[8][kV]; };
     __device__ static constexpr int first_of(int ks, int kg) { return ks * 32 + kg * 8; }
+    template <bool ONCE>
     __device__ static void key(Key& k, const uint8_t* row, const uint8_t*, int kg) {
 #pragma unroll
         for (int i = 0; i < kK; ++i)
-            k.w[i] = once<u32x4>(row + i * 64 + kg * 16);
+            k.w[i] = load<ONCE, u32x4>(row + i * 64 + kg * 16);
     }
     template <typename M>
     __device__ static u32x4 key_of(const Key& k, int ks) { return k.w[ks]; }
+    template <bool ONCE>
     __device__ static void val(Val& v, int i, const uint8_t* row, const uint8_t*, int m) {
         if constexpr (kV == 2) {
-            const u32x2 w = once<u32x2>(row + m * 8);
+            const u32x2 w = load<ONCE, u32x2>(row + m * 8);
             v.w[i][0] = w[0];
             v.w[i][1] = w[1];
         } else {
 #pragma unroll
             for (int j = 0; j < kV; j += 4) {
-                const u32x4 w = once<u32x4>(row + m * (4 * kV) + 4 * j);
+                const u32x4 w = load<ONCE, u32x4>(row + m * (4 * kV) + 4 * j);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v.w[i][j + e] = w[e];
             }
@@ -64,6 +66,11 @@ struct Load16 {
     __device__ static void clear(Val& v, int i) {
 #pragma unroll
         for (int j = 0; j < kV; ++j) v.w[i][j] = 0;
+    }
+    template <typename M>
+    __device__ static void tame(Val& v, int i, bool* odd) {
+#pragma unroll
+        for (int j = 0; j < kV; ++j) v.w[i][j] = finite_or_zero<M>(v.w[i][j], odd);
     }
     template <typename M>
     __device__ static void vals_of(const Val& v, u32x4 (&out)[E]) {
@@ -116,6 +123,17 @@ struct Load<kFP8, D> {
     __device__ static void clear(Val& v, int i) {
 #pragma unroll
         for (int j = 0; j < kV; ++j) v.w[i][j] = 0;
+    }
+    template <typename M>
+    __device__ static void tame(Val& v, int i, bool* odd) {
+#pragma unroll
+        for (int j = 0; j < kV; ++j)
+#pragma unroll
+            for (int b = 0; b < 32; b += 8)
+                if ((v.w[i][j] >> b & 0x7fu) == 0x7fu) {   // NaN, e4m3's only such value
+                    v.w[i][j] &= ~(0xffu << b);
+                    *odd = true;
+                }
     }
     // Bytes of two tokens are paired before they are widened: one permutation and
     // two conversions for four values.
@@ -186,6 +204,14 @@ struct Load<kInt4, D> {
     __device__ static void clear(Val& v, int i) {
         v.pair[i] = 0;
     }
+    // (A pair that is not finite leaves no finite value in its group.)
+    template <typename M>
+    __device__ static void tame(Val& v, int i, bool* odd) {
+        if ((v.pair[i] & 0x7c00u) == 0x7c00u || (v.pair[i] >> 16 & 0x7c00u) == 0x7c00u) {
+            v.pair[i] = 0;
+            *odd = true;
+        }
+    }
     // Words of two tokens are paired by halves; a shift and a mask then leave the same
     // value of both in the two halves of a register, and one packed fma with their
     // scales and bases makes the operand.
@@ -244,20 +270,23 @@ struct Direct {
             vb[i] = c.block(t + 16 * i + 4 * (lane / 16));
         }
     }
+    template <bool ONCE>
     __device__ void fetch_keys(const Cache& c, uint32_t t, int lane) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            L::key(keys[i],
-                   c.keys + kb[i] * c.chunk + ((t + 16 * i + lane % 16) & c.mask) * kRow, nullptr,
-                   lane / 16);
+            L::template key<ONCE>(
+                keys[i], c.keys + kb[i] * c.chunk + ((t + 16 * i + lane % 16) & c.mask) * kRow,
+                nullptr, lane / 16);
     }
+    template <bool ONCE>
     __device__ void fetch_vals(const Cache& c, uint32_t t, int lane) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint8_t* r =
                 c.vals + vb[i] * c.chunk + ((t + 16 * i + 4 * (lane / 16)) & c.mask) * kRow;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) L::val(vals, 4 * i + j, r + j * kRow, nullptr, lane % 16);
+            for (int j = 0; j < 4; ++j)
+                L::template val<ONCE>(vals, 4 * i + j, r + j * kRow, nullptr, lane % 16);
         }
     }
     __device__ void settle(uint8_t*, int) {}
@@ -297,28 +326,30 @@ struct Staged {
 #pragma unroll
         for (int j = 0; j < kPairPieces; ++j) pb[j] = c.block(t + pair_row_of(j, lane));
     }
+    template <bool ONCE>
     __device__ void fetch_keys(const Cache& c, uint32_t t, int lane) {
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
             const uint64_t at = b[j] * c.chunk + ((t + row_of(j, lane)) & c.mask) * kRow +
                                 (j * 64 + lane) % (kRow / 16) * 16;
-            k[j] = once<u32x4>(c.keys + at);
-            v[j] = once<u32x4>(c.vals + at);
+            k[j] = load<ONCE, u32x4>(c.keys + at);
+            v[j] = load<ONCE, u32x4>(c.vals + at);
         }
 #pragma unroll
         for (int j = 0; j < kPairPieces; ++j) {
             const uint64_t at = pb[j] * c.chunk + ((t + pair_row_of(j, lane)) & c.mask) * kPairs +
                                 (j * 64 + lane) % kRowPairs * kPair;
             if constexpr (kPair == 16) {
-                kp[j] = once<u32x4>(c.kpairs + at);
-                vp[j] = once<u32x4>(c.vpairs + at);
+                kp[j] = load<ONCE, u32x4>(c.kpairs + at);
+                vp[j] = load<ONCE, u32x4>(c.vpairs + at);
             } else {
-                const u32x2 x = once<u32x2>(c.kpairs + at), y = once<u32x2>(c.vpairs + at);
+                const u32x2 x = load<ONCE, u32x2>(c.kpairs + at), y = load<ONCE, u32x2>(c.vpairs + at);
                 kp[j] = u32x4{x[0], x[1], 0, 0};
                 vp[j] = u32x4{y[0], y[1], 0, 0};
             }
         }
     }
+    template <bool ONCE>
     __device__ void fetch_vals(const Cache&, uint32_t, int) {}
     __device__ void settle(uint8_t* lds, int lane) {
         // A wave's LDS instructions are done in their order; the fences keep the compiler
@@ -369,9 +400,11 @@ struct Source<kInt4, D> : Staged<kInt4, D, D == 64 ? 64 : 32> {};   // whole pie
 
 // Q: type of the queries and the result.  M: type of the products: fp16 for a 4-bit
 // pool, whose values are fp16 numbers.
-// Two waves a SIMD at least, where their registers allow it (heads up to 128).
+// Three waves a SIMD, where their registers allow it (heads up to 128): one was left
+// to two of them by three registers, and took 50 instead of 45 us for 64 chats in 4
+// bits.
 template <int POOL, typename Q, int D>
-__global__ __launch_bounds__(256, D > 128 ? 1 : 2) void rows_kernel(const KvAttend a) {
+__global__ __launch_bounds__(256, D > 128 ? 1 : 3) void rows_kernel(const KvAttend a) {
     using M = std::conditional_t<POOL == kInt4, f16, Q>;
     using L = Load<POOL, D>;
     using S = Source<POOL, D>;
@@ -431,108 +464,116 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void rows_kernel(const KvAtte
     bool odd = false;
     S src;
 
-    uint32_t t = part.begin + wave * kStep;
-    if (t < part.end) {
-        src.blocks(cache, t, lane);
-        src.fetch_keys(cache, t, lane);
-        src.fetch_vals(cache, t, lane);
-        src.blocks(cache, t + kWaves * kStep, lane);
-    }
-    for (; t < part.end; t += kWaves * kStep) {
-        const uint32_t next = t + kWaves * kStep;
-        const bool more = next < part.end;
-        src.settle(lds, lane);
-        if (S::kStaged && more) {
-            src.fetch_keys(cache, next, lane);
-            src.blocks(cache, next + kWaves * kStep, lane);
+    const auto steps = [&](auto once) __attribute__((always_inline)) {
+        constexpr bool kOnce = decltype(once)::value;
+        uint32_t t = part.begin + wave * kStep;
+        if (t < part.end) {
+            src.blocks(cache, t, lane);
+            src.template fetch_keys<kOnce>(cache, t, lane);
+            src.template fetch_vals<kOnce>(cache, t, lane);
+            src.blocks(cache, t + kWaves * kStep, lane);
         }
-        f32x4 s[kTiles];
+        for (; t < part.end; t += kWaves * kStep) {
+            const uint32_t next = t + kWaves * kStep;
+            const bool more = next < part.end;
+            src.settle(lds, lane);
+            if (S::kStaged && more) {
+                src.template fetch_keys<kOnce>(cache, next, lane);
+                src.blocks(cache, next + kWaves * kStep, lane);
+            }
+            f32x4 s[kTiles];
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-            s[i] = f32x4{0, 0, 0, 0};
-            const typename L::Key key = src.key(lds, i, lane);
+            for (int i = 0; i < kTiles; ++i) {
+                s[i] = f32x4{0, 0, 0, 0};
+                const typename L::Key key = src.key(lds, i, lane);
 #pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks)
-                s[i] = Mat<M>::mfma16(
-                    __builtin_bit_cast(V8, L::template key_of<M>(key, ks)), qf[ks], s[i]);
-        }
-        if (!S::kStaged && more) src.fetch_keys(cache, next, lane);
+                for (int ks = 0; ks < D / 32; ++ks)
+                    s[i] = Mat<M>::mfma16(
+                        __builtin_bit_cast(V8, L::template key_of<M>(key, ks)), qf[ks], s[i]);
+            }
+            if (!S::kStaged && more) src.template fetch_keys<kOnce>(cache, next, lane);
 
-        // Tokens behind a column's limit, or another part's, get no weight.
-        const uint32_t stop = min(limit, part.end);
-        const bool masked = t + kStep > min(least, part.end);
-        if (masked)
+            // Tokens behind a column's limit, or another part's, get no weight.
+            const uint32_t stop = min(limit, part.end);
+            const bool masked = t + kStep > min(least, part.end);
+            if (masked)
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (t + 16 * i + S::token(kg, r) >= stop) s[i][r] = -__builtin_inff();
+            float high = -__builtin_inff();
 #pragma unroll
             for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (t + 16 * i + S::token(kg, r) >= stop) s[i][r] = -__builtin_inff();
-        float high = -__builtin_inff();
+                for (int r = 0; r < 4; ++r) high = fmaxf(high, s[i][r]);
+            high = over_rows(high, Max()) * scale2;
+            if (__any(high > top + kSlack)) {
+                // (A column that has seen nothing keeps its -inf, and sums of 0.)
+                const float raised = fmaxf(top, high);
+                const float f = raised > -__builtin_inff() ? exp2_(top - raised) : 1.0f;
+                top = raised;
+                sum *= f;
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) high = fmaxf(high, s[i][r]);
-        high = over_rows(high, Max()) * scale2;
-        if (__any(high > top + kSlack)) {
-            // (A column that has seen nothing keeps its -inf, and sums of 0.)
-            const float raised = fmaxf(top, high);
-            const float f = raised > -__builtin_inff() ? exp2_(top - raised) : 1.0f;
-            top = raised;
-            sum *= f;
-#pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] *= f;
-        }
-        const float off = top > -__builtin_inff() ? top - kLift : 0.0f;
-#pragma unroll
-        for (int half = 0; half < kTiles / 2; ++half) {
-            // Where the products' type is no finer than the result's, weights are in two
-            // terms, the second what the first's rounding left: the products have time to
-            // spare, and the result is as exact as its own rounding.
-            u32x4 pw, pr = {0, 0, 0, 0};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float x = exp2_(__builtin_fmaf(s[2 * half + i / 2][i % 2 * 2], scale2, -off));
-                const float y =
-                    exp2_(__builtin_fmaf(s[2 * half + i / 2][i % 2 * 2 + 1], scale2, -off));
-                sum += x + y;
-                const uint32_t w = pack2<M>(x, y);
-                pw[i] = w;
-                if (kTwo) pr[i] = pack2<M>(x - lo_float<M>(w), y - hi_float<M>(w));
+                for (int e = 0; e < E; ++e) acc[e] *= f;
             }
-            const V8 pf = __builtin_bit_cast(V8, pw), pg = __builtin_bit_cast(V8, pr);
+            const float off = top > -__builtin_inff() ? top - kLift : 0.0f;
+#pragma unroll
+            for (int half = 0; half < kTiles / 2; ++half) {
+                // Where the products' type is no finer than the result's, weights are in two
+                // terms, the second what the first's rounding left: the products have time to
+                // spare, and the result is as exact as its own rounding.
+                u32x4 pw, pr = {0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = exp2_(__builtin_fmaf(s[2 * half + i / 2][i % 2 * 2], scale2, -off));
+                    const float y =
+                        exp2_(__builtin_fmaf(s[2 * half + i / 2][i % 2 * 2 + 1], scale2, -off));
+                    sum += x + y;
+                    const uint32_t w = pack2<M>(x, y);
+                    pw[i] = w;
+                    if (kTwo) pr[i] = pack2<M>(x - lo_float<M>(w), y - hi_float<M>(w));
+                }
+                const V8 pf = __builtin_bit_cast(V8, pw), pg = __builtin_bit_cast(V8, pr);
 
-            typename L::Val val = src.val(lds, half, lane);
-            if (masked) {
-                // What stands behind the context may be anything: no weight is no help
-                // against NaN.
+                typename L::Val val = src.val(lds, half, lane);
+                if (masked) {
+                    // What stands behind the context may be anything: no weight is no help
+                    // against NaN.
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (t + 32 * half + i / 4 * 16 + S::token(kg, i % 4) >= seq.context)
-                        L::clear(val, i);
+                    for (int i = 0; i < 8; ++i)
+                        if (t + 32 * half + i / 4 * 16 + S::token(kg, i % 4) >= seq.context)
+                            L::clear(val, i);
+                        else if (seq.fresh > 1)
+                            L::template tame<M>(val, i, &odd);
+                }
+                u32x4 vf[E];
+                L::template vals_of<M>(val, vf);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    acc[e] = Mat<M>::mfma16(__builtin_bit_cast(V8, vf[e]), pf, acc[e]);
+                if (kTwo)
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        acc[e] = Mat<M>::mfma16(__builtin_bit_cast(V8, vf[e]), pg, acc[e]);
             }
-            u32x4 vf[E];
-            L::template vals_of<M>(val, vf);
-            if (masked && seq.fresh > 1)
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-#pragma unroll
-                    for (int p = 0; p < 4; ++p) vf[e][p] = finite_or_zero<M>(vf[e][p], &odd);
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                acc[e] = Mat<M>::mfma16(__builtin_bit_cast(V8, vf[e]), pf, acc[e]);
-            if (kTwo)
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    acc[e] = Mat<M>::mfma16(__builtin_bit_cast(V8, vf[e]), pg, acc[e]);
+            if (!S::kStaged && more) {
+                src.template fetch_vals<kOnce>(cache, next, lane);
+                src.blocks(cache, next + kWaves * kStep, lane);
+            }
         }
-        if (!S::kStaged && more) {
-            src.fetch_vals(cache, next, lane);
-            src.blocks(cache, next + kWaves * kStep, lane);
-        }
-    }
+    };
+    // Loads that tell that no other workgroup reads the data leave the caches to others:
+    // 64 chats in bf16 took 91 instead of 102 us.  Where several tiles of columns share
+    // a context they would read it from memory each: 32 columns took 98 instead of
+    // 74 us.
+    if (columns <= kRowColumns)
+        steps(std::true_type());
+    else
+        steps(std::false_type());
 
     if (__any(odd))
-        for (t = part.begin + wave * kStep; t < part.end; t += kWaves * kStep) {
+        for (uint32_t t = part.begin + wave * kStep; t < part.end; t += kWaves * kStep) {
             if (t + kStep <= min(least, part.end)) continue;
             for (uint32_t k = t; k < min(t + kStep, part.end); ++k) {
                 const uint64_t at = cache.block(k) * cache.chunk;
