@@ -570,14 +570,17 @@ AQUA_API aqua_status aqua_cfs_partition(const aqua_cfs_request* requests,
  * graph uses whatever the batch was last set to before each replay (on the
  * replay's stream, or ordered before it), so one graph serves every step;
  * its launches are as wide as the batch's limits, so keep those near.  A
- * captured append must be given a rotation table of as many rows as the
- * longest context that a replay will meet: rows behind the table are not
- * rotated but left unwritten.  aqua_kv_batch_set is refused on a stream that
- * is being captured.
+ * captured call's tensors have max_tokens rows, and a captured append's rotation table as
+ * many as the longest context that a replay will meet: tokens behind the table
+ * are left unwritten.  A replayed append writes nothing where the call itself would
+ * return AQUA_ERR_DUPLICATE.  aqua_kv_batch_set is refused on a stream that is being
+ * captured.
  *
  * Limits: block_tokens a power of two from 4 to 1024; head_dim 64, 128 or 256;
  * num_q_heads a multiple of the pool's num_kv_heads, at most 65536; a context of
- * at most 2^30 tokens. */
+ * at most 2^30 tokens; max_seqs up to 2^20, max_tokens up to 2^22, max_blocks up to
+ * 2^28, and a launch of fewer than 2^32 threads (max_tokens * num_q_heads up to 2^23
+ * keeps it there). */
 typedef struct aqua_kv_batch* aqua_kv_batch_t;
 
 typedef struct {

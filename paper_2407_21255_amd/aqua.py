@@ -718,7 +718,14 @@ class KVBatch:
     def set(self, tables, context, new, stream=None) -> None:
         """``tables`` as for swaps; ``context``: tokens of each sequence, the new ones
         among them; ``new``: how many of them are new."""
-        ids, offs = _csr(tables)
+        if isinstance(tables, list) and tables and \
+                all(isinstance(t, np.ndarray) for t in tables):
+            # (As _csr does, without a Python number for every block.)
+            ids = np.ascontiguousarray(np.concatenate(tables), dtype=np.int32)
+            offs = np.zeros(len(tables) + 1, dtype=np.uint64)
+            offs[1:] = np.cumsum([len(t) for t in tables])
+        else:
+            ids, offs = _csr(tables)
         ctx, fresh = (np.ascontiguousarray(x, dtype=np.int64) for x in (context, new))
         if not len(ctx) == len(fresh) == len(offs) - 1 or \
                 (len(ctx) and (min(ctx.min(), fresh.min()) < 0 or ctx.max() >= 1 << 32)):

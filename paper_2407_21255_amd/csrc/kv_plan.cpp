@@ -70,7 +70,7 @@ aqua_status kv_limits(const Shape& s, const aqua_kv_batch_desc* d, KvLimits* out
     if (!d->num_q_heads || d->num_q_heads > 65536 || d->num_q_heads % s.H)
         return AQUA_ERR_INVALID;
     if (!d->max_seqs || !d->max_tokens || !d->max_blocks) return AQUA_ERR_INVALID;
-    if (d->max_seqs > (1u << 24) || d->max_tokens > (1u << 28) || d->max_blocks > (1u << 28))
+    if (d->max_seqs > (1u << 20) || d->max_tokens > (1u << 22) || d->max_blocks > (1u << 28))
         return AQUA_ERR_INVALID;
     KvLimits m;
     m.shape = s;
@@ -98,8 +98,10 @@ aqua_status kv_limits(const Shape& s, const aqua_kv_batch_desc* d, KvLimits* out
     // turns <= p / kJoinAhead + 1 (and groups / turns rounded down: twice that).
     const uint64_t joins =
         (row_slots + tile_slots) * (kRowColumns + join_groups(s.D)) / join_groups(s.D) + 16;
-    if (most_rows * H > 0x7fffffffull || most_tiles * H > 0x7fffffffull ||
-        joins * H > 0x7fffffffull || (row_slots + tile_slots) * H > 0x7fffffffull)
+    // A launch has fewer than 2^32 threads, 256 or 512 a workgroup; columns are counted in
+    // 32 bits.
+    if (most_rows * H >= (1ull << 24) || most_tiles * H >= (1ull << 23) ||
+        joins * H >= (1ull << 31) || G * m.tokens >= (1ull << 31))
         return AQUA_ERR_INVALID;
     m.rows = (uint32_t)most_rows;
     m.tiles = (uint32_t)most_tiles;

@@ -178,8 +178,12 @@ def test_what_a_batch_refuses():
                  (1, 64, 2, 16, 96, BF16), (1, 64, 2, 16, 32, BF16), (1, 64, 2, 16, 512, BF16)]:
         assert limits(pool, (4, 1, 1, 1))[0] == INVALID, pool
     for batch in [(3, 1, 1, 1), (0, 1, 1, 1), (4, 0, 1, 1), (4, 1, 0, 1), (4, 1, 1, 0),
-                  (65538, 1, 1, 1), (4, (1 << 24) + 1, 1, 1), (4, 1, (1 << 28) + 1, 1)]:
+                  (65538, 1, 1, 1), (4, (1 << 20) + 1, 1, 1), (4, 1, (1 << 22) + 1, 1),
+                  (4, 1, 1, (1 << 28) + 1), (65536, 1 << 20, 1 << 22, 1)]:
         assert limits(ok, batch)[0] == INVALID, batch
+    # As large as the header promises.
+    for H, Hq, tokens in [(1, 64, 1 << 17), (64, 64, 1 << 17), (1, 2, 1 << 22), (8, 8, 1 << 20)]:
+        assert limits((1, 64, H, 16, 128, BF16), (Hq, min(tokens, 1 << 20), tokens, 1))[0] == OK
 
 
 def test_what_a_step_refuses():
