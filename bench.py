@@ -39,16 +39,16 @@ HOST_LINK_PEAK_GBS = 63.0    # PCIe 5.0 x16, one direction, after encoding
 # or to how they are launched reports null until measured again.
 # Recorded with the profile summary of the same kernel under profiles/.
 MEASURED_TRAFFIC = {
-    ("llama70b_hbm", "d24b03372800018f"): {
-        "gather (swap-out)": 21475424356, "scatter (swap-in)": 21475302416},
-    ("llama8b_hbm", "d24b03372800018f"): {
-        "gather (swap-out)": 4295551990, "scatter (swap-in)": 4295161554},
-    ("llama70b_tp2_hbm", "d24b03372800018f"): {
-        "gather (swap-out)": 10739663424, "scatter (swap-in)": 10737802395},
-    ("llama70b_tp4_hbm", "d24b03372800018f"): {
-        "gather (swap-out)": 5369068990, "scatter (swap-in)": 5368998292},
-    ("llama8b_fp8_hbm", "d24b03372800018f"): {
-        "gather (swap-out)": 2147884844, "scatter (swap-in)": 2147674162},
+    ("llama70b_hbm", "703579014f1ddc5a"): {
+        "gather (swap-out)": 21475425856, "scatter (swap-in)": 21475301782},
+    ("llama8b_hbm", "703579014f1ddc5a"): {
+        "gather (swap-out)": 4295556714, "scatter (swap-in)": 4295157190},
+    ("llama70b_tp2_hbm", "703579014f1ddc5a"): {
+        "gather (swap-out)": 10739648424, "scatter (swap-in)": 10737805998},
+    ("llama70b_tp4_hbm", "703579014f1ddc5a"): {
+        "gather (swap-out)": 5369077158, "scatter (swap-in)": 5368999207},
+    ("llama8b_fp8_hbm", "703579014f1ddc5a"): {
+        "gather (swap-out)": 2147883796, "scatter (swap-in)": 2147663172},
 }
 
 # Every source that decides what the swap kernels do and how they are
