@@ -26,20 +26,28 @@ constexpr uint32_t kRowColumns = 16;
 // wave's sums take twice the registers.
 constexpr uint32_t tile_columns(uint32_t head_dim) { return head_dim > 128 ? 128 : 256; }
 
-// Up to this many columns go to the rows kernel.
+// Up to this many columns go to the rows kernel.  Measured with 32 contexts of 128 to
+// 8192 tokens and 8 KV heads, us: rows with 16, 32 and 64 columns 56, 74 and 110; tiles
+// with 72 and 128 columns 109 and 123.
 constexpr uint32_t kRowsMostColumns = 64;
 
 // How a kernel's items are split into parts of at most `most` tokens (part_tokens):
 //   wide     workgroups that run at once;
 //   step     tokens that a workgroup takes in a step: parts are whole ones;
-//   fewest   tokens of a part that is worth a join (see kRows, kTiles);
+//   fewest   tokens of a part that is worth a join;
 //   rounds   workgroups are at most `wide` times this, but for those of whole items;
 //   start    what starting a part costs, in tokens.
+// Measured on MI355X, us.  Rows, parts of 256 / 512 / 1024 tokens at least: one chat of
+// 512 tokens 14.6 / 11.6 / 11.5 (a join is a launch more), three documents of 30001 to
+// 131072 on one KV head 23.6 / 23.5 / 25.5, 64 chats the same.  `start` 64 / 192: 64
+// chats in 8 bits 55 / 58, in 4 bits 55 / 53, in bf16 92 / 91.  Tiles, 512 tokens and a
+// start of 128 / 128 and 256: a chunk of 100 tokens behind 4000 34.4 / 31.3, 1000 tokens
+// of 64 heads 42.7 / 39.9, six prompts of 300 to 700 41.0 / 42.9.
 struct KvSplit {
     uint32_t wide, step, fewest, rounds, start;
 };
 constexpr KvSplit kRows{512, 256, 512, 8, 64};
-constexpr KvSplit kTiles{256, 64, 512, 4, 128};
+constexpr KvSplit kTiles{256, 64, 256, 4, 256};
 
 constexpr uint32_t kMostContext = 1u << 30;
 constexpr uint32_t kNoSlot = 0xffffffffu;
