@@ -566,6 +566,11 @@ AQUA_API aqua_status aqua_cfs_partition(const aqua_cfs_request* requests,
  * of graphs that captured them among them, share its device tables and its
  * split sums: those that may overlap in time need a batch each, or one stream.
  *
+ * Threads: a batch is used from one thread at a time.
+ *
+ * Errors: argument errors are found before anything is enqueued, as everywhere.
+ * AQUA_ERR_HIP if memory cannot be had or a launch fails.
+ *
  * Capture: aqua_kv_append and aqua_kv_attend may be captured into a graph.  The
  * graph uses whatever the batch was last set to before each replay (on the
  * replay's stream, or ordered before it), so one graph serves every step;

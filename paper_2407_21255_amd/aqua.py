@@ -761,12 +761,13 @@ class KVBatch:
     def _used(stream, *tensors) -> None:
         """Tensors of torch's allocator that another than the current stream uses are
         not handed out again before it is done with them."""
-        if stream is None or isinstance(stream, int):
+        if stream is None:
             return
-        if stream.cuda_stream != torch.cuda.current_stream(stream.device).cuda_stream:
+        s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+        if s.cuda_stream != torch.cuda.current_stream(s.device).cuda_stream:
             for t in tensors:
                 if t is not None:
-                    t.record_stream(stream)
+                    t.record_stream(s)
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor,
                q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,

@@ -21,8 +21,9 @@ uint64_t parts_of(const std::vector<uint32_t>& ends, uint64_t most) {
 // of `wide` ends after r parts of the longest size, or the work of all spread evenly
 // and one part more, whichever is less; every round starts its parts anew.  For each
 // number of rounds the smallest parts that fit them are found by bisection, and
-// the rounds that end first are taken.
-uint64_t part_tokens(const std::vector<uint32_t>& ends, uint32_t H, const KvSplit& sp) {
+// the rounds that end first are taken.  `bits`: of a value.
+uint64_t part_tokens(const std::vector<uint32_t>& ends, uint32_t H, const KvSplit& sp,
+                     uint32_t bits) {
     uint64_t work = 0, longest = 0;
     for (uint32_t e : ends) {
         work += (uint64_t)H * e;
@@ -31,9 +32,9 @@ uint64_t part_tokens(const std::vector<uint32_t>& ends, uint32_t H, const KvSpli
     if (longest <= sp.fewest) return sp.fewest;
     const uint64_t whole = ceil_div(longest, sp.step) * sp.step, even = ceil_div(work, sp.wide);
     const auto cost = [&](uint64_t rounds, uint64_t most) {
-        return std::min(rounds * most, even + most) + rounds * sp.start;
+        return std::min(rounds * most, even + most) + rounds * sp.start * 16 / bits;
     };
-    uint64_t best = whole, least = cost(ceil_div(ends.size() * (uint64_t)H, sp.wide), whole);
+    uint64_t best = whole, least = cost(ceil_div(ends.size() * (uint64_t)H, sp.wide), longest);
     for (uint64_t r = 1; r <= sp.rounds; ++r) {
         const uint64_t fit = r * sp.wide;
         if (ends.size() * (uint64_t)H > fit) continue;
@@ -45,7 +46,7 @@ uint64_t part_tokens(const std::vector<uint32_t>& ends, uint32_t H, const KvSpli
             else
                 lo = mid + 1;
         }
-        const uint64_t c = cost(r, hi * sp.step);
+        const uint64_t c = cost(r, hi * sp.step) + sp.join * 16 / bits;
         if (c < least) {
             least = c;
             best = hi * sp.step;
@@ -175,6 +176,7 @@ aqua_status kv_plan(const KvLimits& lim, uint32_t num_seqs, const int32_t* ids,
     const auto wide = [&](const KvSeq& q) {
         return (uint64_t)G * q.fresh > kRowsMostColumns && lim.tiles;
     };
+    const uint32_t bits = (uint32_t)(lim.shape.C * 8 / (2ull * H * T * lim.shape.D));
     plan->slots = 0;
     for (int w = 0; w < 2; ++w) {
         const KvSplit& sp = w ? kTiles : kRows;
@@ -186,7 +188,7 @@ aqua_status kv_plan(const KvLimits& lim, uint32_t num_seqs, const int32_t* ids,
                 for (uint64_t t = 0; t * columns < (uint64_t)G * q.fresh; ++t)
                     plan->ends.push_back(tile_end(q, G, columns, (uint32_t)t));
         if (plan->ends.empty()) continue;
-        const uint64_t most = part_tokens(plan->ends, H, sp);
+        const uint64_t most = part_tokens(plan->ends, H, sp, w ? 16 : bits);
         for (const KvSeq& q : plan->seqs) {
             if (!q.fresh || wide(q) != (w == 1)) continue;
             const uint64_t all = (uint64_t)G * q.fresh;

@@ -36,18 +36,22 @@ constexpr uint32_t kRowsMostColumns = 64;
 //   step     tokens that a workgroup takes in a step: parts are whole ones;
 //   fewest   tokens of a part that is worth a join;
 //   rounds   workgroups are at most `wide` times this, but for those of whole items;
-//   start    what starting a part costs, in tokens.
+//   start    what starting a part costs, and
+//   join     what a launch that joins costs, in tokens (of 16 bits, where reading the
+//            tokens is what takes the time: scaled by a pool's own).
 // Measured on MI355X, us.  Rows, parts of 256 / 512 / 1024 tokens at least: one chat of
 // 512 tokens 14.6 / 11.6 / 11.5 (a join is a launch more), three documents of 30001 to
-// 131072 on one KV head 23.6 / 23.5 / 25.5, 64 chats the same.  `start` 64 / 192: 64
-// chats in 8 bits 55 / 58, in 4 bits 55 / 53, in bf16 92 / 91.  Tiles, 512 tokens and a
-// start of 128 / 128 and 256: a chunk of 100 tokens behind 4000 34.4 / 31.3, 1000 tokens
-// of 64 heads 42.7 / 39.9, six prompts of 300 to 700 41.0 / 42.9.
+// 131072 on one KV head 23.6 / 23.5 / 25.5, 64 chats the same.  `start` 64 / 320: 64
+// chats in bf16 91 / 94, in 4 bits 47 / 42 (there 64 and 205 are one); 256 chats of up to
+// 600 tokens, joined because nothing said what a join costs, 38, and left whole 35.
+// Tiles, 512 tokens and a start of 128 / 128 and 256: a chunk of 100 tokens behind 4000
+// 34.4 / 31.3, 1000 tokens of 64 heads 42.7 / 39.9, six prompts of 300 to 700
+// 41.0 / 42.9.
 struct KvSplit {
-    uint32_t wide, step, fewest, rounds, start;
+    uint32_t wide, step, fewest, rounds, start, join;
 };
-constexpr KvSplit kRows{512, 256, 512, 8, 64};
-constexpr KvSplit kTiles{256, 64, 256, 4, 256};
+constexpr KvSplit kRows{512, 256, 512, 8, 64, 150};
+constexpr KvSplit kTiles{256, 64, 256, 4, 256, 0};
 
 constexpr uint32_t kMostContext = 1u << 30;
 constexpr uint32_t kNoSlot = 0xffffffffu;
