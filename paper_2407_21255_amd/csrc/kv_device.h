@@ -167,7 +167,7 @@ __device__ inline float odd_value(const uint8_t* row, const uint8_t* pairs, uint
     } else {
         x = (float)*reinterpret_cast<const M*>(row + 2 * d);
     }
-    return x - x == 0.0f ? 0.0f : x;
+    return __builtin_isfinite(x) ? 0.0f : x;
 }
 
 // Queries of type Q as operands of products of type M.  Where Q has more range (bf16

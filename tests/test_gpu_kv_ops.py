@@ -384,6 +384,29 @@ def test_append_strange_values():
                 assert float((got[5] - want[5]).abs().max()) <= 16 * 2.0 ** -25
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -120, 1e-3, 0.3, 7.0, 2.0 ** 120])
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+def test_append_fp8_scales(dt, scale):
+    """The fp32 quotient, rounded to nearest even: every 16-bit pattern, infinities and
+    NaN among them, and halfway cases of the type."""
+    shape = (1, 80, 2, 16, 256, FP8)
+    n = 256
+    with Step(shape, 2, [n], [n], dt, poison=False) as s:
+        x = torch.arange(1 << 16, device="cuda").to(torch.int16).view(dt).view(128, 2, 256)
+        half = (torch.randint(1, 64, (128, 2, 256), device="cuda") * 0.125 * scale).to(dt)
+        v = torch.cat([x, half])
+        s.batch.append(0, v, v.flip(0), k_scale=scale, v_scale=scale)
+        torch.cuda.synchronize()
+        ids = torch.from_numpy(s.tables[0]).long().cuda()
+        got = s.pool.view(torch.float8_e4m3fn).view(80, 2, 2, 16, 256)[ids]
+        got = got.to(F64).permute(1, 2, 0, 3, 4).flatten(2, 3)          # [2, H, n, D]
+        q = v.float() / torch.full_like(v, scale, dtype=torch.float32)   # IEEE division
+        want = q.clamp(-448, 448).to(torch.float8_e4m3fn).to(F64).permute(1, 0, 2)
+        for which, w in ((0, want), (1, want.flip(1))):
+            assert torch.equal(got[which].isnan(), w.isnan())
+            assert torch.equal(got[which].nan_to_num(9.0), w.nan_to_num(9.0))
+
+
 # -- together, as a program uses them --------------------------------------------
 
 @pytest.mark.parametrize("kind", [KINDS[1], KINDS[3], KINDS[4]],
