@@ -215,7 +215,8 @@ aqua_status aqua_kv_batch_create(aqua_kv_pool_t pool, const aqua_kv_batch_desc* 
         (uint64_t)limits.slots * view.shape.H * aqua::slot_floats(view.shape.D) * sizeof(float);
     bool ok = hipMalloc(reinterpret_cast<void**>(&b->device), b->layout.bytes) == hipSuccess &&
               hipMalloc(reinterpret_cast<void**>(&b->slots), slots) == hipSuccess &&
-              hipMemset(b->device, 0, kAlign) == hipSuccess;
+              hipMemset(b->device, 0, kAlign) == hipSuccess &&
+              hipStreamSynchronize(nullptr) == hipSuccess;  // a set's stream may not wait for it
     for (int k = 0; ok && k < kStages; ++k)
         ok = hipHostMalloc(reinterpret_cast<void**>(&b->stage[k]), b->layout.bytes,
                            hipHostMallocMapped | hipHostMallocCoherent) == hipSuccess &&

@@ -229,6 +229,33 @@ def test_offsets_past_32_bits():
         assert int(pool[:2 * N * 32768 + (N - 100) * 32768].count_nonzero()) == 0
 
 
+def test_so_many_heads_that_nothing_is_split():
+    """More KV heads than parts that a launch is split into: no room for split sums."""
+    H, T, D = 8192, 64, 128
+    shape = (1, 1, H, T, D, BF16)
+    pool = torch.zeros(ref.chunk_bytes(*shape[2:]), dtype=torch.uint8, device="cuda")
+    with aqua.KVPool(shape, pool) as kv, aqua.KVBatch(kv, H, 1, 1, 1) as batch:
+        q, k, v = (torch.randn(1, H, D, device="cuda").bfloat16() for _ in range(3))
+        batch.set([np.array([0])], [T], [1])
+        batch.append(0, k, v)
+        out, lse = batch.attend(0, q, lse=True, scale=1.0 / 16)
+        torch.cuda.synchronize()
+        rows = pool.view(torch.bfloat16).view(2, H, T, D)
+        assert torch.equal(rows[0, :, -1], k[0]) and torch.equal(rows[1, :, -1], v[0])
+        assert not bool(rows[:, :, :-1].any())
+        # T - 1 keys of zeros, whose scores are 0, and values of zeros.
+        s = (q[0].to(F64) * k[0].to(F64)).sum(-1) / 16
+        w = s.exp() / (s.exp() + T - 1)
+        want = w[:, None] * v[0].to(F64)
+        # A score's fp32 sum of D products, and T weights' fp32 sum; then the weight's
+        # two 16-bit terms and the result's rounding.
+        score = D * 2.0 ** -24 * (q[0].to(F64) * k[0].to(F64)).abs().sum(-1) / 16
+        off = score + T * 2.0 ** -24
+        assert bool(((lse[0].to(F64) - (s.exp() + T - 1).log()).abs() <= off).all())
+        off = (2 * off + 2.0 ** -16 + 2.0 ** -8)[:, None]
+        assert bool(((out[0].to(F64) - want).abs() <= off * want.abs()).all())
+
+
 def test_attend_twice_gives_the_same_bits():
     ctx, new = [20001, 9000, 33], [1, 300, 1]
     shape = (1, 1900, 2, 16, 128, INT4)
