@@ -646,8 +646,8 @@ typedef struct {
  * base = min - 16 * scale of the group (rounded to fp16 in turn) and
  * code = round((value - base) / scale) - 16, kept within 0..15; a NaN makes its
  * group NaN.  A 16-bit pool takes tensors of its own type, an fp8 or 4-bit pool
- * both.  AQUA_ERR_INVALID for tensors other than described, overlapping q and q_out
- * that are not the same, or a rotation table that is shorter than the longest
+ * both.  AQUA_ERR_INVALID for tensors other than described, a q_out that overlaps k, v or
+ * a q that is not the same, or a rotation table that is shorter than the longest
  * context; AQUA_ERR_DUPLICATE when two tokens of the batch go to blocks
  * that another table of the batch holds too (a shared prefix's blocks can be
  * read, but its last block has to be copied before one of its owners appends). */

@@ -87,17 +87,18 @@ bool tensor_ok(int device, const void* ptr, uint64_t rows, uint64_t heads, uint6
     return !rows || device_range(device, ptr, 2 * ((rows - 1) * stride + heads * D));
 }
 
-// Whether rows of `width` elements at a and b, with strides as and bs, share bytes:
+// Whether rows of aw elements at a and of bw at b, with strides as and bs, share bytes:
 // exact where the strides are equal, else by the tensors' extents.
-bool rows_meet(const void* a, uint64_t as, const void* b, uint64_t bs, uint64_t rows,
-               uint64_t width) {
+bool rows_meet(const void* a, uint64_t as, uint64_t aw, const void* b, uint64_t bs, uint64_t bw,
+               uint64_t rows) {
     if (!rows) return false;
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    if (x + 2 * ((rows - 1) * as + width) <= y || y + 2 * ((rows - 1) * bs + width) <= x)
+    if (x + 2 * ((rows - 1) * as + aw) <= y || y + 2 * ((rows - 1) * bs + bw) <= x)
         return false;
     if (as != bs) return true;
-    const uint64_t apart = (x < y ? y - x : x - y) % (2 * as);
-    return apart < 2 * width || 2 * as - apart < 2 * width;
+    // Bytes from the start of a's row to the start of b's next.
+    const uint64_t apart = x <= y ? (y - x) % (2 * as) : 2 * as - 1 - (x - y - 1) % (2 * as);
+    return apart < 2 * aw || 2 * as - apart < 2 * bw;
 }
 
 bool positive(float x) { return std::isfinite(x) && x > 0.0f; }
@@ -311,9 +312,13 @@ aqua_status aqua_kv_append(aqua_kv_batch_t b, uint32_t layer, const aqua_kv_appe
         if (!tensor_ok(dev, x->q, rows, q_heads, s.D, x->q_stride) ||
             !tensor_ok(dev, x->q_out, rows, q_heads, s.D, x->q_out_stride))
             return AQUA_ERR_INVALID;
+        const uint64_t width = (uint64_t)q_heads * s.D, own = (uint64_t)s.H * s.D;
         const bool in_place = x->q == x->q_out && x->q_stride == x->q_out_stride;
-        if (!in_place && rows_meet(x->q, x->q_stride, x->q_out, x->q_out_stride, rows,
-                                   (uint64_t)q_heads * s.D))
+        const auto meets = [&](const void* p, uint64_t stride, uint64_t w) {
+            return rows_meet(x->q_out, x->q_out_stride, width, p, stride, w, rows);
+        };
+        if ((!in_place && meets(x->q, x->q_stride, width)) || meets(x->k, x->k_stride, own) ||
+            meets(x->v, x->v_stride, own))
             return AQUA_ERR_INVALID;
     }
     if (x->rope) {
@@ -361,7 +366,8 @@ aqua_status aqua_kv_attend(aqua_kv_batch_t b, uint32_t layer, const aqua_kv_atte
     const int dev = b->pool.device;
     if (!tensor_ok(dev, x->q, rows, heads, s.D, x->q_stride) ||
         !tensor_ok(dev, x->out, rows, heads, s.D, x->out_stride) ||
-        rows_meet(x->q, x->q_stride, x->out, x->out_stride, rows, (uint64_t)heads * s.D))
+        rows_meet(x->q, x->q_stride, (uint64_t)heads * s.D, x->out, x->out_stride,
+                  (uint64_t)heads * s.D, rows))
         return AQUA_ERR_INVALID;
     if (x->lse && ((uintptr_t)x->lse % 4 ||
                    (rows && !device_range(dev, x->lse, 4ull * rows * heads))))

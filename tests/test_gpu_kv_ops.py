@@ -593,6 +593,27 @@ def test_another_stream_and_two_batches():
         s.check_attend(0, s.q, "streams", got=got[0])
 
 
+def test_results_on_another_stream_are_its_own_memory():
+    """What the current stream has let go may still be read there: a result on another
+    stream does not lie in it."""
+    with Step((1, 20, 2, 16, 128, BF16), 4, [100, 50], [2, 50], torch.bfloat16) as s:
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        gone = []
+        for shape, dt in [((s.tokens, 4, 128), torch.bfloat16), ((s.tokens, 4), torch.float32)]:
+            t = torch.empty(shape, dtype=dt, device="cuda")
+            gone.append(t.data_ptr())
+            del t
+        q_out = s.batch.append(0, s.k, s.v, q=s.q, stream=side)
+        out, lse = s.batch.attend(0, q_out, lse=True, stream=side)
+        raw = s.batch.attend(0, q_out, stream=side.cuda_stream)
+        side.synchronize()
+        for t in (q_out, out, lse, raw):
+            assert t.data_ptr() not in gone
+        assert torch.equal(q_out, s.q) and torch.equal(raw, out)
+        s.check_attend(0, s.q, "side stream", got=(out, lse))
+
+
 def test_shared_prefix_is_read_by_both():
     """Two sequences whose tables share full blocks; appending to a shared block is
     refused."""
@@ -665,6 +686,11 @@ def test_refusals():
         refused("no queries", lambda: ap(q_out=out))
         refused("queries shifted", lambda: ap(q=s.q, q_out=s.qkv[:, 1:5]))
         refused("v scale", lambda: ap(v_scale=0.5))
+        refused("queries onto keys", lambda: ap(q=s.q.clone(), q_out=s.qkv[:, 1:5]))
+        refused("queries onto values", lambda: ap(q=s.q.clone(), q_out=s.qkv[:, 4:8]))
+        x = torch.zeros(n + 1, 8, 128, dtype=torch.bfloat16, device="cuda")
+        shifted = torch.as_strided(x, (n, 4, 128), x.stride(), 6 * 128)   # 2 heads of the next row
+        refused("queries onto the next row's keys", lambda: ap(k=x[:n, :2], q=s.q, q_out=shifted))
 
         CAP, RANGE = aqua.AQUA_ERR_CAPACITY, aqua.AQUA_ERR_RANGE
         t = s.tables
