@@ -660,7 +660,8 @@ typedef struct {
     float* lse;           /* [tokens][num_q_heads] log of the softmax's sum, or NULL */
     uint64_t q_stride, out_stride;
     int32_t dtype;        /* of q and out: AQUA_F16 or AQUA_BF16 */
-    float scale;          /* of the scores, usually 1 / sqrt(D); finite */
+    float scale;          /* of the scores, usually 1 / sqrt(D); scale * k_scale * log2(e)
+                             is finite in fp32 */
     float k_scale, v_scale; /* fp8 pools: what a stored value is multiplied with */
 } aqua_kv_attend_args;
 

@@ -355,7 +355,8 @@ aqua_status aqua_kv_attend(aqua_kv_batch_t b, uint32_t layer, const aqua_kv_atte
     Range trace("aqua_kv_attend");
     if (!b || !x || layer >= b->pool.shape.L) return AQUA_ERR_INVALID;
     const aqua::Shape& s = b->pool.shape;
-    if (!b->takes(x->dtype) || !b->scales_ok(x->k_scale, x->v_scale) || !std::isfinite(x->scale))
+    const float scale2 = (float)((double)x->scale * x->k_scale * 1.4426950408889634);
+    if (!b->takes(x->dtype) || !b->scales_ok(x->k_scale, x->v_scale) || !std::isfinite(scale2))
         return AQUA_ERR_INVALID;
     const hipStream_t st = (hipStream_t)stream;
     OnDevice on(b->pool.device);
@@ -383,7 +384,7 @@ aqua_status aqua_kv_attend(aqua_kv_batch_t b, uint32_t layer, const aqua_kv_atte
     a.q_heads = heads;
     a.group = b->limits.group;
     a.dtype = x->dtype;
-    a.scale2 = (float)((double)x->scale * x->k_scale * 1.4426950408889634);
+    a.scale2 = scale2;
     a.v_scale = x->v_scale;
     return aqua::launch_attend(a, b->counts(captured), st) == hipSuccess ? AQUA_OK : AQUA_ERR_HIP;
 }

@@ -671,6 +671,8 @@ def test_refusals():
                                                        device="cuda")[1:].view(n, 4, 128)))
         refused("the result is the queries", lambda: at(out=s.q))
         refused("infinite scale", lambda: at(scale=float("inf")))
+        refused("scale past fp32 in powers of two", lambda: at(scale=3e38))
+        refused("no number", lambda: at(scale=float("nan")))
         refused("scale of another pool", lambda: at(k_scale=2.0))
         refused("lse type", lambda: at(lse=torch.zeros(n, 4, device="cuda", dtype=F64)))
         refused("lse rows", lambda: at(lse=torch.zeros(n - 1, 4, device="cuda")))
