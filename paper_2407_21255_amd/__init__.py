@@ -4,6 +4,7 @@ every context switch (Aqua, ASPLOS '25, section 7).
 
 Modules:
   aqua      ctypes binding of the C ABI (include/aqua.h); loads libaqua.so.
+  aqua.KVBatch  the operators on the pool between two swaps (append, attend).
   workload  seeded synthetic inputs (pools, block tables, schedules).
   build     in-tree build of libaqua.so (hipcc, gfx950) and the host core.
 
