@@ -770,15 +770,15 @@ class KVBatch:
                     t.record_stream(s)
 
     @staticmethod
-    def _result(stream, like: torch.Tensor, shape, dtype=None) -> torch.Tensor:
-        """A new tensor that a call on `stream` fills.  It is the memory of that stream: what
-        the current one has let go may still be in use there."""
-        if stream is None:
-            return like.new_empty(shape, dtype=dtype)
+    def _result(stream, like: torch.Tensor, dtype=None) -> torch.Tensor:
+        """A new tensor like `like` that a call on `stream` fills.  It is the memory of that
+        stream: what the current one has let go may still be in use there."""
+        if stream is None:   # (1.2 us; new_empty takes 1.8)
+            return torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
         s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
         current = torch.cuda.current_stream(like.device)
         with torch.cuda.stream(s):
-            t = like.new_empty(shape, dtype=dtype)
+            t = torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
         if s.cuda_stream != current.cuda_stream:
             t.record_stream(current)
         return t
@@ -804,7 +804,7 @@ class KVBatch:
         if q is not None:
             a.q_stride = self._stride(q, self.num_q_heads, rows, name)
             if q_out is None:
-                q_out = self._result(stream, q, q.shape)
+                q_out = self._result(stream, q)
             if q_out.dtype != q.dtype:
                 raise AquaError(AQUA_ERR_INVALID, name)
             a.q_out_stride = self._stride(q_out, self.num_q_heads, rows, name)
@@ -835,11 +835,11 @@ class KVBatch:
         rows = self._needed(stream)
         stride = self._stride(q, self.num_q_heads, rows, name)
         if out is None:
-            out = self._result(stream, q, q.shape)
+            out = self._result(stream, q)
         if out.dtype != q.dtype:
             raise AquaError(AQUA_ERR_INVALID, name)
         if lse is True:
-            lse = self._result(stream, q, q.shape[:2], torch.float32)
+            lse = self._result(stream, q[:, :, 0], torch.float32)
         elif lse is False:
             lse = None
         if lse is not None and (lse.dtype != torch.float32 or lse.dim() != 2
