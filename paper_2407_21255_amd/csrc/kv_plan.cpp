@@ -10,47 +10,65 @@ namespace {
 
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
-// An item to split: its tokens.
-uint64_t parts_of(const std::vector<uint32_t>& ends, uint64_t most) {
-    uint64_t n = 0;
-    for (uint32_t e : ends) n += ceil_div(e, most);
-    return n;
-}
-
-// Tokens of a part at most.  Workgroups start longest first, so a launch of r rounds
-// of `wide` ends after r parts of the longest size, or the work of all spread evenly
-// and one part more, whichever is less; every round starts its parts anew.  For each
-// number of rounds the smallest parts that fit them are found by bisection, and
-// the rounds that end first are taken.  `bits`: of a value.
-uint64_t part_tokens(const std::vector<uint32_t>& ends, uint32_t H, const KvSplit& sp,
-                     uint32_t bits) {
+// Tokens of a part at most, for items of `ends` tokens (whose order is not kept).
+// Workgroups start longest first, so a launch of r rounds of `wide` ends after r parts of
+// the longest size, or the work of all spread evenly and one part more, whichever is less;
+// every round starts its parts anew.  For each number of rounds, from what whole items
+// take on, the smallest parts that fit them are found by bisection, and the rounds that
+// end first are taken.  More than sp.rounds are looked at only where a part is still
+// longer than all the work spread evenly, which the other workgroups cannot hide: one
+// long context among so many short ones that these fill the rounds by themselves.
+// `bits`: of a value; at most `most_items` items come of it, and `most_parts` parts of
+// items that are split.
+uint64_t part_tokens(std::vector<uint32_t>& ends, uint32_t H, const KvSplit& sp, uint32_t bits,
+                     uint64_t most_items, uint64_t most_parts) {
     uint64_t work = 0, longest = 0;
     for (uint32_t e : ends) {
         work += (uint64_t)H * e;
         longest = std::max<uint64_t>(longest, e);
     }
     if (longest <= sp.fewest) return sp.fewest;
+    // Those that may be split, first: often few.
+    const auto split = std::partition(ends.begin(), ends.end(),
+                                      [&](uint32_t e) { return e > sp.fewest; });
+    const auto fits = [&](uint32_t most, uint64_t added) {
+        uint64_t parts = 0;
+        for (auto e = ends.begin(); e != split; ++e) {
+            if (*e <= most) continue;
+            const uint32_t n = (*e + most - 1) / most;
+            parts += n;
+            if (parts > most_parts || n - 1 > added) return false;
+            added -= n - 1;
+        }
+        return true;
+    };
+    const uint64_t n = ends.size(), first = ceil_div(n * H, sp.wide);
     const uint64_t whole = ceil_div(longest, sp.step) * sp.step, even = ceil_div(work, sp.wide);
     const auto cost = [&](uint64_t rounds, uint64_t most) {
         return std::min(rounds * most, even + most) + rounds * sp.start * 16 / bits;
     };
-    uint64_t best = whole, least = cost(ceil_div(ends.size() * (uint64_t)H, sp.wide), longest);
-    for (uint64_t r = 1; r <= sp.rounds; ++r) {
-        const uint64_t fit = r * sp.wide;
-        if (ends.size() * (uint64_t)H > fit) continue;
-        uint64_t lo = sp.fewest / sp.step, hi = whole / sp.step;  // hi fits
+    const uint64_t join = sp.join * 16 / bits;
+    uint64_t best = whole, least = cost(first, longest);
+    uint64_t hi = whole / sp.step;  // fits
+    for (uint64_t r = first; r < first + sp.rounds; ++r) {
+        if (r > sp.rounds && best <= even) break;
+        if (cost(r, sp.fewest) + join >= least) break;  // nor do more rounds end before
+        const uint64_t items = std::min(most_items, r * sp.wide / H);
+        if (items < n) continue;
+        uint64_t lo = sp.fewest / sp.step;
         while (lo < hi) {
             const uint64_t mid = (lo + hi) / 2;
-            if (parts_of(ends, mid * sp.step) * H <= fit)
+            if (fits((uint32_t)(mid * sp.step), items - n))
                 hi = mid;
             else
                 lo = mid + 1;
         }
-        const uint64_t c = cost(r, hi * sp.step) + sp.join * 16 / bits;
+        const uint64_t c = cost(r, hi * sp.step) + join;
         if (c < least) {
             least = c;
             best = hi * sp.step;
         }
+        if (hi == sp.fewest / sp.step) break;
     }
     return best;
 }
@@ -81,8 +99,8 @@ aqua_status kv_limits(const Shape& s, const aqua_kv_batch_desc* d, KvLimits* out
     m.blocks = d->max_blocks;
     m.group = m.q_heads / s.H;
     const uint64_t G = m.group, H = s.H;
-    // Items of whole contexts: a sequence's columns round up to a tile.  Splitting makes
-    // at most wide * rounds workgroups of the items that it is used for.
+    // Items of whole contexts: a sequence's columns round up to a tile.  The parts of those
+    // that are split are at most wide * rounds workgroups.
     const uint64_t busy = std::min(m.seqs, m.tokens);
     const uint64_t wide = std::min<uint64_t>(busy, G * m.tokens / (kRowsMostColumns + 1));
     const uint32_t tc = tile_columns(s.D);
@@ -91,23 +109,25 @@ aqua_status kv_limits(const Shape& s, const aqua_kv_batch_desc* d, KvLimits* out
     // (A single token's heads may be more columns than kRowsMostColumns; they go to
     // the tiles kernel, whose items are fewer.)
     const uint64_t tiles = wide ? wide + G * m.tokens / tc : 0;
-    const uint64_t row_slots = kRows.wide * kRows.rounds / H;
-    const uint64_t tile_slots = tiles ? kTiles.wide * kTiles.rounds / H * (tc / kRowColumns) : 0;
-    const uint64_t most_rows = std::max(rows, row_slots);
-    const uint64_t most_tiles = tiles ? std::max<uint64_t>(tiles, kTiles.wide * kTiles.rounds / H) : 0;
+    const uint64_t row_parts = kRows.wide * kRows.rounds / H;
+    const uint64_t tile_parts = tiles ? kTiles.wide * kTiles.rounds / H : 0;
+    const uint64_t tile_slots = tile_parts * (tc / kRowColumns);
     // A tile of 16 with p >= 2 parts makes at most 1 + 16 turns / groups joins, with
     // turns <= p / kJoinAhead + 1 (and groups / turns rounded down: twice that).
     const uint64_t joins =
-        (row_slots + tile_slots) * (kRowColumns + join_groups(s.D)) / join_groups(s.D) + 16;
+        (row_parts + tile_slots) * (kRowColumns + join_groups(s.D)) / join_groups(s.D) + 16;
     // A launch has fewer than 2^32 threads, 256 or 512 a workgroup; columns are counted in
     // 32 bits.
-    if (most_rows * H >= (1ull << 24) || most_tiles * H >= (1ull << 23) ||
+    const uint64_t row_room = ((1ull << 24) - 1) / H, tile_room = ((1ull << 23) - 1) / H;
+    if (rows > row_room || tiles > tile_room ||
         joins * H >= (1ull << 31) || G * m.tokens >= (1ull << 31))
         return AQUA_ERR_INVALID;
-    m.rows = (uint32_t)most_rows;
-    m.tiles = (uint32_t)most_tiles;
+    m.rows = (uint32_t)std::min(rows + row_parts, row_room);
+    m.tiles = (uint32_t)std::min(tiles + tile_parts, tile_room);
+    m.row_parts = (uint32_t)row_parts;
+    m.tile_parts = (uint32_t)tile_parts;
     m.joins = (uint32_t)joins;
-    m.slots = (uint32_t)(row_slots + tile_slots);
+    m.slots = (uint32_t)(row_parts + tile_slots);
     *out = m;
     return AQUA_OK;
 }
@@ -188,7 +208,9 @@ aqua_status kv_plan(const KvLimits& lim, uint32_t num_seqs, const int32_t* ids,
                 for (uint64_t t = 0; t * columns < (uint64_t)G * q.fresh; ++t)
                     plan->ends.push_back(tile_end(q, G, columns, (uint32_t)t));
         if (plan->ends.empty()) continue;
-        const uint64_t most = part_tokens(plan->ends, H, sp, w ? 16 : bits);
+        const uint64_t most =
+            w ? part_tokens(plan->ends, H, sp, 16, lim.tiles, lim.tile_parts)
+              : part_tokens(plan->ends, H, sp, bits, lim.rows, lim.row_parts);
         for (const KvSeq& q : plan->seqs) {
             if (!q.fresh || wide(q) != (w == 1)) continue;
             const uint64_t all = (uint64_t)G * q.fresh;

@@ -35,7 +35,11 @@ constexpr uint32_t kRowsMostColumns = 64;
 //   wide     workgroups that run at once;
 //   step     tokens that a workgroup takes in a step: parts are whole ones;
 //   fewest   tokens of a part that is worth a join;
-//   rounds   workgroups are at most `wide` times this, but for those of whole items;
+//   rounds   parts of split items are at most `wide` times this many workgroups, and so are
+//            all together, but where whole items take as many by themselves and a part
+//            would be longer than all the work spread evenly: then splitting adds fewer
+//            than this many rounds (600 contexts of 100 tokens and one of 131072, 8 KV
+//            heads of 128: 148 us, and with the long one whole 1893);
 //   start    what starting a part costs, and
 //   join     what a launch that joins costs, in tokens (of 16 bits, where reading the
 //            tokens is what takes the time: scaled by a pool's own).
@@ -98,6 +102,7 @@ struct KvLimits {
     uint32_t q_heads = 0, seqs = 0, tokens = 0, blocks = 0;
     uint32_t group = 0;                         // G
     uint32_t rows = 0, tiles = 0, joins = 0;    // work items
+    uint32_t row_parts = 0, tile_parts = 0;     // of them, parts of items that are split
     uint32_t slots = 0;                         // groups of H slots of 16 columns
 };
 

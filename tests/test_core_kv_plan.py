@@ -219,3 +219,42 @@ def test_four_bit_chunks():
     assert v((2, 4, 2, 4, 64, INT4), 2 * 640) == OK
     for desc in [(1, 4, 8, 16, 80, INT4), (1, 4, 8, 16, 16, INT4), (1, 4, 1, 1, 32, INT4)]:
         assert v(desc, 1 << 20) == INVALID, desc
+
+
+def _mixed(H, Hq, short, long, new, D=128):
+    """`short` contexts of 100 tokens and one long one, with `new` tokens each."""
+    T, rng = 16, np.random.default_rng(short)
+    ctx = [100] * short + [long]
+    ctx = [int(x) for x in rng.permutation(ctx)]
+    fresh = [min(c, new) for c in ctx]
+    blocks = sum(-(-c // T) for c in ctx)
+    pool = (1, blocks, H, T, D, BF16)
+    batch = (Hq, len(ctx), sum(fresh), blocks)
+    tables = _tables(ctx, T, blocks, rng)
+    st, lim = limits(pool, batch)
+    assert st == OK
+    st, p = plan(pool, batch, tables, ctx, fresh)
+    assert st == OK
+    _check_cover(pool, batch, np.cumsum([0] + [len(t) for t in tables])[:-1].tolist(), ctx,
+                 fresh, p, lim)
+    return p
+
+
+@pytest.mark.parametrize("H,short", [(8, 63), (8, 500), (8, 511), (8, 600), (8, 4000), (32, 128),
+                                     (32, 600), (1, 5000)])
+def test_a_long_context_among_many_short_ones_is_split(H, short):
+    """Whatever whole items there are beside it: no part is longer than what a
+    workgroup has to do when the work is spread evenly."""
+    p = _mixed(H, 32, short, 131072, 1)
+    longest = int((p["rows"][:, 6].astype(int) - p["rows"][:, 5]).max())
+    even = -(-(short * 100 + 131072) * H // 512)
+    assert longest <= max(512, -(-even // 256) * 256)
+
+
+@pytest.mark.parametrize("short", [20, 101, 128, 400])
+@pytest.mark.parametrize("D,columns", [(128, 256), (256, 128)])
+def test_a_chunk_behind_a_long_context_beside_many_prompts_is_split(D, columns, short):
+    p = _mixed(8, 32, short, 131072, 100, D)
+    n = p["tiles"][:, 6].astype(int) - p["tiles"][:, 5]
+    even = -(-int(n.sum()) * 8 // 256)
+    assert int(n.max()) <= max(256, -(-even // 64) * 64)

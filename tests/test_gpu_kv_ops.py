@@ -734,3 +734,25 @@ def test_refusals():
         with aqua.KVPool(shape, pool) as kv:
             with pytest.raises(aqua.AquaError):
                 aqua.KVBatch(kv, 4, 1, 1, 1)
+
+
+# -- a step's shape ----------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", [KINDS[1], KINDS[4]], ids=[KIND_IDS[1], KIND_IDS[4]])
+def test_a_long_context_among_many_short_ones(kind):
+    """So many short contexts that they fill a launch's rounds by themselves, and one that
+    is split all the same; called and captured."""
+    ctx = [1 + (37 * i) % 61 for i in range(530)]
+    ctx[200] = 20011
+    shape = (1, sum(-(-c // 16) for c in ctx) + 3, 8, 16, 64, kind[0])
+    with Step(shape, 24, ctx, [1] * len(ctx), kind[1], seed=5) as s:
+        out, lse = s.check_attend(0, s.q, "many")
+        graph, again = torch.cuda.CUDAGraph(), torch.empty_like(out)
+        with torch.cuda.graph(graph):
+            s.batch.attend(0, s.q, out=again)
+        for _ in range(3):
+            again.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(again, out)
+        del graph
