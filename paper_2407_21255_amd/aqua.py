@@ -421,17 +421,36 @@ def _addr(a: Optional[np.ndarray]) -> Optional[int]:
     return None if a is None else a.__array_interface__["data"][0]
 
 
+_INT32, _INT64, _UINT64 = (np.dtype(t) for t in (np.int32, np.int64, np.uint64))
+
+
+def _whole(a, dtype: np.dtype, status: int, what: str) -> np.ndarray:
+    """Numbers in a row as an array of `dtype`, none of them wrapped or cut on the way."""
+    a = np.asarray(a)
+    if a.dtype is not dtype:
+        with np.errstate(invalid="ignore"):
+            b = a.astype(dtype)
+        if not np.array_equal(b, a):
+            raise AquaError(status, what)
+        a = b
+    if a.ndim != 1:
+        raise AquaError(AQUA_ERR_INVALID, what)
+    return np.ascontiguousarray(a)
+
+
 def _csr(tables):
     """(int32 ids, uint64 offsets) from a list of tables or an (ids, offs) pair."""
     if isinstance(tables, tuple) and len(tables) == 2 and isinstance(tables[0], np.ndarray):
-        ids, offs = tables
-    else:
-        ids = np.asarray([b for t in tables for b in t], dtype=np.int32)
-        offs = np.zeros(len(tables) + 1, dtype=np.uint64)
-        if len(tables):
-            offs[1:] = np.cumsum([len(t) for t in tables])
-    return (np.ascontiguousarray(ids, dtype=np.int32),
-            np.ascontiguousarray(offs, dtype=np.uint64))
+        ids = _whole(tables[0], _INT32, AQUA_ERR_RANGE, "block ids")
+        offs = _whole(tables[1], _UINT64, AQUA_ERR_INVALID, "table offsets")
+        if not len(offs) or offs.item(-1) > len(ids):
+            raise AquaError(AQUA_ERR_INVALID, "table offsets")
+        return ids, offs
+    ids = np.asarray([b for t in tables for b in t], dtype=np.int32)
+    offs = np.zeros(len(tables) + 1, dtype=np.uint64)
+    if len(tables):
+        offs[1:] = np.cumsum([len(t) for t in tables])
+    return _whole(ids, _INT32, AQUA_ERR_RANGE, "block ids"), offs
 
 
 # The current device's current stream as a handle, without the Stream object
@@ -703,6 +722,8 @@ class KVBatch:
 
     def __init__(self, pool: "KVPool", num_q_heads: int, max_seqs: int, max_tokens: int,
                  max_blocks: int):
+        if not all(0 <= x < 1 << 32 for x in (num_q_heads, max_seqs, max_tokens, max_blocks)):
+            raise AquaError(AQUA_ERR_INVALID, "aqua_kv_batch_create")
         st, h = aqua_kv_batch_create(
             pool.handle, aqua_kv_batch_desc(num_q_heads, max_seqs, max_tokens, max_blocks))
         if st != AQUA_OK:
@@ -721,12 +742,17 @@ class KVBatch:
         if isinstance(tables, list) and tables and \
                 all(isinstance(t, np.ndarray) for t in tables):
             # (As _csr does, without a Python number for every block.)
-            ids = np.ascontiguousarray(np.concatenate(tables), dtype=np.int32)
+            try:
+                ids = np.concatenate(tables)
+            except ValueError:   # tables that are not rows of numbers all
+                raise AquaError(AQUA_ERR_INVALID, "aqua_kv_batch_set") from None
+            ids = _whole(ids, _INT32, AQUA_ERR_RANGE, "aqua_kv_batch_set")
             offs = np.zeros(len(tables) + 1, dtype=np.uint64)
             offs[1:] = np.cumsum([len(t) for t in tables])
         else:
             ids, offs = _csr(tables)
-        ctx, fresh = (np.ascontiguousarray(x, dtype=np.int64) for x in (context, new))
+        ctx, fresh = (_whole(x, _INT64, AQUA_ERR_INVALID, "aqua_kv_batch_set")
+                      for x in (context, new))
         if not len(ctx) == len(fresh) == len(offs) - 1 or \
                 (len(ctx) and (min(ctx.min(), fresh.min()) < 0 or ctx.max() >= 1 << 32)):
             raise AquaError(AQUA_ERR_INVALID, "aqua_kv_batch_set")
@@ -736,6 +762,10 @@ class KVBatch:
         if st != AQUA_OK:
             raise AquaError(st, "aqua_kv_batch_set")
         self.tokens = int(fresh.sum())
+
+    def _check_layer(self, layer: int, what: str) -> None:
+        if not 0 <= layer < self.pool.desc.num_layers:   # (ctypes takes a number's low bits)
+            raise AquaError(AQUA_ERR_INVALID, what)
 
     def _needed(self, stream) -> int:
         """Rows that a call's tensors have: the step's, or, for a call that is being
@@ -792,6 +822,7 @@ class KVBatch:
         and then sines.  Returns the rotated queries (``q_out``, which may be ``q``
         itself, or a new tensor), None without ``q``."""
         name, H = "aqua_kv_append", self.pool.desc.num_kv_heads
+        self._check_layer(layer, name)
         dtype = _DTYPES.get(k.dtype)
         if dtype is None or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
             raise AquaError(AQUA_ERR_INVALID, name)
@@ -829,6 +860,7 @@ class KVBatch:
         a contiguous float32 tensor [tokens, query heads] to fill; then (out, lse) is
         returned, else out."""
         name = "aqua_kv_attend"
+        self._check_layer(layer, name)
         dtype = _DTYPES.get(q.dtype)
         if dtype is None:
             raise AquaError(AQUA_ERR_INVALID, name)
