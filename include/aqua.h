@@ -597,7 +597,15 @@ typedef struct {
 
 /* Allocates the batch's device tables and workspace and its pinned staging
  * memory.  AQUA_ERR_INVALID for a pool or limits outside those above.  The
- * batch keeps the pool's shape and memory address, and not the pool. */
+ * batch keeps the pool's shape and memory address, and not the pool.
+ *
+ * Device memory: the tables, about 4 bytes a table entry, 8 a token and 32 for each
+ * part that contexts are split into, and four pinned copies of them; and the split
+ * sums of contexts that are split over workgroups, 64 * (head_dim + 2) bytes for 16
+ * (new token, query head) pairs of a KV head and part.  max_blocks bounds those: none where
+ * max_blocks * block_tokens is at most 256; at most 35 MB for heads of 128 (17 for 64, 68
+ * for 256) where max_tokens * num_q_heads / num_kv_heads is at most 64, and 171 (87, 203)
+ * beyond, where prompts may be split too.  Every batch has its own. */
 AQUA_API aqua_status aqua_kv_batch_create(aqua_kv_pool_t pool, const aqua_kv_batch_desc* desc,
                                           aqua_kv_batch_t* out);
 

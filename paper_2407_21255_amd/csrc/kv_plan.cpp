@@ -99,8 +99,7 @@ aqua_status kv_limits(const Shape& s, const aqua_kv_batch_desc* d, KvLimits* out
     m.blocks = d->max_blocks;
     m.group = m.q_heads / s.H;
     const uint64_t G = m.group, H = s.H;
-    // Items of whole contexts: a sequence's columns round up to a tile.  The parts of those
-    // that are split are at most wide * rounds workgroups.
+    // Items of whole contexts: a sequence's columns round up to a tile.
     const uint64_t busy = std::min(m.seqs, m.tokens);
     const uint64_t wide = std::min<uint64_t>(busy, G * m.tokens / (kRowsMostColumns + 1));
     const uint32_t tc = tile_columns(s.D);
@@ -109,13 +108,27 @@ aqua_status kv_limits(const Shape& s, const aqua_kv_batch_desc* d, KvLimits* out
     // (A single token's heads may be more columns than kRowsMostColumns; they go to
     // the tiles kernel, whose items are fewer.)
     const uint64_t tiles = wide ? wide + G * m.tokens / tc : 0;
-    const uint64_t row_parts = kRows.wide * kRows.rounds / H;
-    const uint64_t tile_parts = tiles ? kTiles.wide * kTiles.rounds / H : 0;
+    // The parts of items that are split are at most wide * rounds workgroups, and no more
+    // than the tables' tokens make.  A context of e > fewest tokens has at most e / fewest + 1
+    // parts for each of its items; rows items are one for each 16 of its columns, which
+    // are at most kRowsMostColumns.
+    const uint64_t held = (uint64_t)m.blocks * s.T;
+    const uint64_t row_items =
+        ceil_div(std::min<uint64_t>(G * m.tokens, kRowsMostColumns), kRowColumns);
+    const uint64_t row_parts =
+        held > kRows.fewest
+            ? std::min(row_items * (held / kRows.fewest + std::min(busy, held / (kRows.fewest + 1))),
+                       (uint64_t)kRows.wide * kRows.rounds / H)
+            : 0;
+    const uint64_t tile_parts =
+        held > kTiles.fewest ? std::min(tiles * ceil_div(held, kTiles.fewest),
+                                        (uint64_t)kTiles.wide * kTiles.rounds / H)
+                             : 0;
     const uint64_t tile_slots = tile_parts * (tc / kRowColumns);
     // A tile of 16 with p >= 2 parts makes at most 1 + 16 turns / groups joins, with
     // turns <= p / kJoinAhead + 1 (and groups / turns rounded down: twice that).
-    const uint64_t joins =
-        (row_parts + tile_slots) * (kRowColumns + join_groups(s.D)) / join_groups(s.D) + 16;
+    const uint64_t slots = row_parts + tile_slots, groups = join_groups(s.D);
+    const uint64_t joins = slots ? slots * (kRowColumns + groups) / groups + 16 : 0;
     // A launch has fewer than 2^32 threads, 256 or 512 a workgroup; columns are counted in
     // 32 bits.
     const uint64_t row_room = ((1ull << 24) - 1) / H, tile_room = ((1ull << 23) - 1) / H;
@@ -127,7 +140,7 @@ aqua_status kv_limits(const Shape& s, const aqua_kv_batch_desc* d, KvLimits* out
     m.row_parts = (uint32_t)row_parts;
     m.tile_parts = (uint32_t)tile_parts;
     m.joins = (uint32_t)joins;
-    m.slots = (uint32_t)(row_parts + tile_slots);
+    m.slots = (uint32_t)slots;
     *out = m;
     return AQUA_OK;
 }

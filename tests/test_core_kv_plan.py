@@ -258,3 +258,56 @@ def test_a_chunk_behind_a_long_context_beside_many_prompts_is_split(D, columns, 
     n = p["tiles"][:, 6].astype(int) - p["tiles"][:, 5]
     even = -(-int(n.sum()) * 8 // 256)
     assert int(n.max()) <= max(256, -(-even // 64) * 64)
+
+
+def _workspace(pool, lim):
+    """Bytes of split sums: 16 columns of D values, maxima and totals a slot and KV head."""
+    return lim["slots"] * pool[2] * 16 * (pool[4] + 2) * 4
+
+
+def test_the_workspace_is_what_a_split_of_the_batchs_blocks_can_need():
+    pool = (1, 1 << 20, 8, 16, 128, BF16)
+    # Contexts that are never split: 32 blocks hold 512 tokens, 16 hold 256.
+    for batch in [(32, 1, 1, 1), (32, 1, 1, 32), (32, 64, 16, 32), (32, 1, 64, 4), (32, 1, 512, 16)]:
+        st, lim = limits(pool, batch)
+        assert st == OK and lim["slots"] == lim["joins"] == 0, batch
+    # One more block, and there are two parts; more grow with it.
+    st, lim = limits(pool, (32, 1, 1, 33))
+    assert st == OK and 2 <= lim["slots"] <= 4
+    st, more = limits(pool, (32, 1, 1, 330))
+    assert lim["slots"] < more["slots"] <= 40
+    # Decode batches take no room for prompts' tiles; at most what the header says.
+    for D, rows, tiles in ((64, 17.4e6, 69.3e6), (128, 34.1e6, 136.4e6), (256, 67.7e6, 135.3e6)):
+        big = (1, 1 << 20, 8, 16, D, BF16)
+        assert 0.99 * rows < _workspace(big, limits(big, (32, 16, 16, 1 << 20))[1]) <= rows
+        assert 0.99 * (rows + tiles) < _workspace(big, limits(big, (32, 64, 64, 1 << 20))[1]) <= \
+            rows + tiles
+
+
+@pytest.mark.parametrize("heads", [(8, 32), (1, 71), (5, 5), (2, 64)])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_room_for_the_batchs_blocks_takes_no_part_from_a_step(heads, D):
+    """A step is planned alike in a batch that just holds its tables and in a larger one."""
+    H, Hq = heads
+    rng = np.random.default_rng(H * 7 + D)
+    for trial in range(40):
+        T = int(rng.choice([4, 16, 256]))
+        n = int(rng.integers(1, 12))
+        ctx = [int(x) for x in np.exp(rng.uniform(0, np.log(120000 if trial % 2 else 3000), n))]
+        if trial % 5 == 0:
+            ctx = [int(x) for x in rng.choice([256, 257, 512, 513, 768, 1024, 1025], n)]
+        new = [1 if trial % 3 == 0 else int(rng.integers(0, min(c, 5) + 1)) if trial % 3 == 1
+               else int(rng.integers(0, min(c, 300) + 1)) for c in ctx]
+        if not sum(new):
+            continue
+        tables = _tables(ctx, T, sum(-(-c // T) for c in ctx) + n, rng)
+        blocks = sum(len(t) for t in tables)
+        pool = (2, blocks + n, H, T, D, BF16)
+        exact, wide = (Hq, n, sum(new), blocks), (Hq, n, sum(new), blocks + (1 << 20))
+        st, lim = limits(pool, exact)
+        (sa, a), (sb, b) = plan(pool, exact, tables, ctx, new), plan(pool, wide, tables, ctx, new)
+        assert st == sa == sb == OK
+        for name in ("rows", "tiles", "joins", "tokens"):
+            assert np.array_equal(a[name], b[name]), (trial, name)
+            assert len(a[name]) <= lim.get(name, 1 << 32)
+        assert a["counts"]["slots"] <= lim["slots"]
