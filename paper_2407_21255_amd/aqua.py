@@ -718,7 +718,8 @@ class KVBatch:
     aqua_kv_batch_create): ``set`` once a step, then ``append`` and ``attend`` for
     every layer.  Tensors are [tokens, heads, head_dim] device tensors of one 16-bit
     type, their heads contiguous, the new tokens of all sequences packed in
-    sequence order.  Closed with its pool at the latest."""
+    sequence order.  There is no backward pass: tensors that require a gradient are
+    refused where gradients are on.  Closed with its pool at the latest."""
 
     def __init__(self, pool: "KVPool", num_q_heads: int, max_seqs: int, max_tokens: int,
                  max_blocks: int):
@@ -766,6 +767,16 @@ class KVBatch:
     def _check_layer(self, layer: int, what: str) -> None:
         if not 0 <= layer < self.pool.desc.num_layers:   # (ctypes takes a number's low bits)
             raise AquaError(AQUA_ERR_INVALID, what)
+
+    @staticmethod
+    def _no_gradients(what: str, *tensors) -> None:
+        """The operators have no backward pass: a result that silently has no gradient
+        would cut the caller's graph."""
+        if torch.is_grad_enabled():
+            for t in tensors:
+                if t is not None and t.requires_grad:
+                    raise AquaError(AQUA_ERR_INVALID, what + ", which makes no gradient, of a "
+                                    "tensor that requires one (detach it, or use torch.no_grad())")
 
     def _needed(self, stream) -> int:
         """Rows that a call's tensors have: the step's, or, for a call that is being
@@ -823,6 +834,7 @@ class KVBatch:
         itself, or a new tensor), None without ``q``."""
         name, H = "aqua_kv_append", self.pool.desc.num_kv_heads
         self._check_layer(layer, name)
+        self._no_gradients(name, k, v, q, q_out, rope)
         dtype = _DTYPES.get(k.dtype)
         if dtype is None or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
             raise AquaError(AQUA_ERR_INVALID, name)
@@ -861,6 +873,7 @@ class KVBatch:
         returned, else out."""
         name = "aqua_kv_attend"
         self._check_layer(layer, name)
+        self._no_gradients(name, q, out, None if isinstance(lse, bool) else lse)
         dtype = _DTYPES.get(q.dtype)
         if dtype is None:
             raise AquaError(AQUA_ERR_INVALID, name)

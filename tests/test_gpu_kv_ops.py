@@ -756,3 +756,21 @@ def test_a_long_context_among_many_short_ones(kind):
             torch.cuda.synchronize()
             assert torch.equal(again, out)
         del graph
+
+
+def test_tensors_of_a_model_under_no_grad():
+    """A model's parameters require gradients; what it makes under no_grad does not, and a
+    leaf is read there as any other tensor."""
+    with Step((1, 40, 2, 16, 128, BF16), 4, [200, 90], [2, 80], torch.bfloat16) as s:
+        leaf = s.q.clone().requires_grad_()
+        with pytest.raises(aqua.AquaError, match="gradient"):
+            s.batch.attend(0, leaf)
+        with torch.no_grad():
+            got = s.batch.attend(0, leaf, lse=True)
+            assert s.batch.append(0, s.k, s.v, q=leaf).equal(leaf)
+        with torch.inference_mode():
+            again = s.batch.attend(0, leaf, lse=True)
+        torch.cuda.synchronize()
+        assert not got[0].requires_grad
+        want = s.batch.attend(0, leaf.detach(), lse=True)
+        assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])

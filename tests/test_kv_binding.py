@@ -112,3 +112,18 @@ def test_numbers_that_32_bits_do_not_hold(monkeypatch):
         with pytest.raises(aqua.AquaError) as e:
             aqua.KVBatch(pool, *args)
         assert e.value.status == INVALID
+
+
+def test_tensors_that_require_a_gradient_are_refused():
+    """A result without a gradient would cut the caller's graph without a word."""
+    x = torch.zeros(1, 2, 128, dtype=torch.bfloat16)
+    q = torch.zeros(1, 4, 128, dtype=torch.bfloat16)
+    rope = torch.zeros(8, 128)
+    g = lambda t: t.clone().requires_grad_()
+    for call in (lambda b: b.append(0, g(x), x), lambda b: b.append(0, x, g(x) * 2),
+                 lambda b: b.append(0, x, x, q=g(q)), lambda b: b.append(0, x, x, q=q, q_out=g(q)),
+                 lambda b: b.append(0, x, x, rope=g(rope)), lambda b: b.attend(0, g(q)),
+                 lambda b: b.attend(0, q, out=g(q)), lambda b: b.attend(0, q, lse=g(rope[:, :4]))):
+        with pytest.raises(aqua.AquaError, match="gradient") as e:
+            call(batch())
+        assert e.value.status == INVALID
