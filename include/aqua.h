@@ -654,9 +654,10 @@ typedef struct {
  * base = min - 16 * scale of the group (rounded to fp16 in turn) and
  * code = round((value - base) / scale) - 16, kept within 0..15; a NaN makes its
  * group NaN.  A 16-bit pool takes tensors of its own type, an fp8 or 4-bit pool
- * both.  AQUA_ERR_INVALID for tensors other than described, a q_out that overlaps k, v or
- * a q that is not the same, or a rotation table that is shorter than the longest
- * context; AQUA_ERR_DUPLICATE when two tokens of the batch go to blocks
+ * both.  AQUA_ERR_INVALID for tensors other than described, a q_out that overlaps k, v,
+ * the rotation table, the pool or a q that is not the same, or a rotation table that is
+ * shorter than the longest context (k, v and q may be the pool's memory, of blocks that
+ * the call does not write); AQUA_ERR_DUPLICATE when two tokens of the batch go to blocks
  * that another table of the batch holds too (a shared prefix's blocks can be
  * read, but its last block has to be copied before one of its owners appends). */
 AQUA_API aqua_status aqua_kv_append(aqua_kv_batch_t batch, uint32_t layer,
@@ -664,8 +665,9 @@ AQUA_API aqua_status aqua_kv_append(aqua_kv_batch_t batch, uint32_t layer,
 
 typedef struct {
     const void* q;        /* [tokens][num_q_heads][D], strided and aligned as above */
-    void* out;            /* the same shape; must not overlap q */
-    float* lse;           /* [tokens][num_q_heads] log of the softmax's sum, or NULL */
+    void* out;            /* the same shape; must not overlap q or the pool */
+    float* lse;           /* [tokens][num_q_heads] log of the softmax's sum, or NULL; must not
+                             lie within q, out (or between their rows) or the pool */
     uint64_t q_stride, out_stride;
     int32_t dtype;        /* of q and out: AQUA_F16 or AQUA_BF16 */
     float scale;          /* of the scores, usually 1 / sqrt(D); scale * k_scale * log2(e)

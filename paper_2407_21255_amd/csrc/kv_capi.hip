@@ -101,6 +101,17 @@ bool rows_meet(const void* a, uint64_t as, uint64_t aw, const void* b, uint64_t 
     return apart < 2 * aw || 2 * as - apart < 2 * bw;
 }
 
+// Bytes of a tensor from its first element to its last.
+uint64_t extent(uint64_t rows, uint64_t stride, uint64_t width) {
+    return rows ? 2 * ((rows - 1) * stride + width) : 0;
+}
+
+// Whether [a, a + an) and [b, b + bn) share bytes.
+bool bytes_meet(const void* a, uint64_t an, const void* b, uint64_t bn) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return an && bn && x < y + bn && y < x + an;
+}
+
 bool positive(float x) { return std::isfinite(x) && x > 0.0f; }
 
 bool capturing(hipStream_t stream) {
@@ -318,13 +329,16 @@ aqua_status aqua_kv_append(aqua_kv_batch_t b, uint32_t layer, const aqua_kv_appe
             return rows_meet(x->q_out, x->q_out_stride, width, p, stride, w, rows);
         };
         if ((!in_place && meets(x->q, x->q_stride, width)) || meets(x->k, x->k_stride, own) ||
-            meets(x->v, x->v_stride, own))
+            meets(x->v, x->v_stride, own) ||
+            bytes_meet(x->q_out, extent(rows, x->q_out_stride, width), b->pool.base, s.pool_bytes))
             return AQUA_ERR_INVALID;
     }
     if (x->rope) {
         if (!x->rope_dim || x->rope_dim % 16 || x->rope_dim > s.D || (uintptr_t)x->rope % 16 ||
             x->rope_rows < b->plan.longest ||
-            !device_range(dev, x->rope, 4ull * x->rope_rows * x->rope_dim))
+            !device_range(dev, x->rope, 4ull * x->rope_rows * x->rope_dim) ||
+            (x->q && bytes_meet(x->q_out, extent(rows, x->q_out_stride, (uint64_t)q_heads * s.D),
+                                x->rope, 4ull * x->rope_rows * x->rope_dim)))
             return AQUA_ERR_INVALID;
     }
     if (!b->plan.append_ok) return AQUA_ERR_DUPLICATE;
@@ -365,13 +379,17 @@ aqua_status aqua_kv_attend(aqua_kv_batch_t b, uint32_t layer, const aqua_kv_atte
     const uint32_t rows = captured ? b->limits.tokens : b->plan.new_tokens;
     const uint32_t heads = b->limits.q_heads;
     const int dev = b->pool.device;
+    const uint64_t width = (uint64_t)heads * s.D;
     if (!tensor_ok(dev, x->q, rows, heads, s.D, x->q_stride) ||
         !tensor_ok(dev, x->out, rows, heads, s.D, x->out_stride) ||
-        rows_meet(x->q, x->q_stride, (uint64_t)heads * s.D, x->out, x->out_stride,
-                  (uint64_t)heads * s.D, rows))
+        rows_meet(x->q, x->q_stride, width, x->out, x->out_stride, width, rows))
         return AQUA_ERR_INVALID;
-    if (x->lse && ((uintptr_t)x->lse % 4 ||
-                   (rows && !device_range(dev, x->lse, 4ull * rows * heads))))
+    const uint64_t out_bytes = extent(rows, x->out_stride, width), lse_bytes = 4ull * rows * heads;
+    if (bytes_meet(x->out, out_bytes, b->pool.base, s.pool_bytes)) return AQUA_ERR_INVALID;
+    if (x->lse && ((uintptr_t)x->lse % 4 || (rows && !device_range(dev, x->lse, lse_bytes)) ||
+                   bytes_meet(x->lse, lse_bytes, x->out, out_bytes) ||
+                   bytes_meet(x->lse, lse_bytes, x->q, extent(rows, x->q_stride, width)) ||
+                   bytes_meet(x->lse, lse_bytes, b->pool.base, s.pool_bytes)))
         return AQUA_ERR_INVALID;
     aqua::KvAttend a;
     a.t = b->tables();

@@ -774,3 +774,58 @@ def test_tensors_of_a_model_under_no_grad():
         assert not got[0].requires_grad
         want = s.batch.attend(0, leaf.detach(), lse=True)
         assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])
+
+
+def test_results_that_share_memory_are_refused():
+    """Outputs lie apart from each other, from what a call reads, and from the pool."""
+    shape = (1, 60, 2, 16, 128, BF16)
+    with Step(shape, 4, [100, 50], [2, 50], torch.bfloat16, poison=False) as s:
+        b, n = s.batch, s.tokens
+        q = s.q.contiguous()
+        out, rope = torch.empty_like(q), ref.rope_table(100, 128)
+        before = s.pool.clone()
+        bf16 = lambda t: t.view(torch.bfloat16)[:q.numel()].view(q.shape)
+        f32 = lambda t: t.view(-1)[:2 * 4 * n].view(torch.float32).view(n, 4)
+        last = lambda t: t.view(-1)[-2 * 4 * n:].view(torch.float32).view(n, 4)
+        wide = torch.zeros(n, 12, 128, dtype=torch.bfloat16, device="cuda")
+        calls = {
+            "lse on the result": lambda: b.attend(0, q, out=out, lse=f32(out)),
+            "lse on the result's end": lambda: b.attend(0, q, out=out, lse=last(out)),
+            "lse on the queries": lambda: b.attend(0, q, out=out, lse=f32(q)),
+            "lse on the last queries": lambda: b.attend(0, q, out=out, lse=last(q)),
+            "lse on the pool": lambda: b.attend(0, q, out=out, lse=f32(bf16(s.pool))),
+            "result on the pool": lambda: b.attend(0, q, out=bf16(s.pool)),
+            "result on the pool's end": lambda: b.attend(0, q, out=bf16(s.pool[-2 * q.numel():])),
+            "queries on the pool": lambda: b.append(0, s.k, s.v, q=q, q_out=bf16(s.pool)),
+            "queries on the table": lambda: b.append(
+                0, s.k, s.v, q=q, q_out=bf16(big), rope=big[:100 * 128].view(100, 128)),
+            "queries on the table's end": lambda: b.append(
+                0, s.k, s.v, q=q, q_out=bf16(big[99 * 128:]), rope=big[:100 * 128].view(100, 128)),
+        }
+        big = torch.zeros(100 * 128 + q.numel(), device="cuda")
+        for what, call in calls.items():
+            with pytest.raises(aqua.AquaError) as e:
+                call()
+            say(what, e.value)
+            assert e.value.status == aqua.AQUA_ERR_INVALID, what
+        torch.cuda.synchronize()
+        assert torch.equal(s.pool, before) and not bool(big.any())
+        # Side by side is apart: results and queries in one tensor's heads, the sums and the
+        # result in one allocation, the queries rotated next to their table.
+        wide[:, :4] = q
+        one = torch.zeros(2 * q.numel() + 4 * 4 * n, dtype=torch.uint8, device="cuda")
+        side, sums = one[:2 * q.numel()].view(torch.bfloat16).view(q.shape), \
+            one[2 * q.numel():].view(torch.float32).view(n, 4)
+        want = b.attend(0, q, lse=True)
+        for o, l in ((wide[:, 4:8], None), (side, sums), (wide[:, 8:], sums)):
+            got = b.attend(0, wide[:, :4], out=o, lse=True if l is None else l)
+            torch.cuda.synchronize()
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        big[:100 * 128] = rope.flatten()
+        turned = b.append(0, s.k, s.v, q=q, q_out=bf16(big[100 * 128:]),
+                          rope=big[:100 * 128].view(100, 128))
+        torch.cuda.synchronize()
+        pos = torch.from_numpy(ref.positions(s.ctx, s.new)).cuda()
+        y, size = ref.rotate(q, pos, rope, False)
+        f = size * 3 * 2.0 ** -24
+        ref.assert_within(turned, y, y.abs() * 2.0 ** -8 + f * (1 + 2.0 ** -8), "queries")
