@@ -642,19 +642,23 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 3) void rows_kernel(const KvAtte
         return;
     }
     const uint64_t row = seq.row + oc_all / G, h = head * G + oc_all % G;
-    const float norm = a.v_scale / total;
+    // (The values' scale by itself: over the sum it may be too small for fp32.)
+    const float norm = 1.0f / total;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= norm;
     uint8_t* out = a.out + 2 * (row * a.out_stride + h * D + od);
     if constexpr (E == 4) {
         *reinterpret_cast<u32x2*>(out) =
-            u32x2{pack2<Q>(o[0] * norm, o[1] * norm), pack2<Q>(o[2] * norm, o[3] * norm)};
+            u32x2{pack2<Q>(o[0] * a.v_scale, o[1] * a.v_scale),
+                  pack2<Q>(o[2] * a.v_scale, o[3] * a.v_scale)};
     } else {
 #pragma unroll
         for (int e = 0; e < E; e += 8)
             *reinterpret_cast<u32x4*>(out + 2 * e) =
-                u32x4{pack2<Q>(o[e] * norm, o[e + 1] * norm),
-                      pack2<Q>(o[e + 2] * norm, o[e + 3] * norm),
-                      pack2<Q>(o[e + 4] * norm, o[e + 5] * norm),
-                      pack2<Q>(o[e + 6] * norm, o[e + 7] * norm)};
+                u32x4{pack2<Q>(o[e] * a.v_scale, o[e + 1] * a.v_scale),
+                      pack2<Q>(o[e + 2] * a.v_scale, o[e + 3] * a.v_scale),
+                      pack2<Q>(o[e + 4] * a.v_scale, o[e + 5] * a.v_scale),
+                      pack2<Q>(o[e + 6] * a.v_scale, o[e + 7] * a.v_scale)};
     }
     if (a.lse && od == 0)
         a.lse[row * a.q_heads + h] = (high - kLift + __builtin_log2f(total)) * kLn2;
@@ -746,9 +750,10 @@ __global__ __launch_bounds__(256) void join_kernel(const KvAttend a) {
         }
         if (!live || turn) continue;
         const uint64_t row = join.row + c / a.group, h = head * a.group + c % a.group;
-        const float norm = a.v_scale / s.total;
+        s.o *= 1.0f / s.total;
         *reinterpret_cast<u32x2*>(a.out + 2 * (row * a.out_stride + h * D + lane * 4)) =
-            u32x2{pack2<Q>(s.o[0] * norm, s.o[1] * norm), pack2<Q>(s.o[2] * norm, s.o[3] * norm)};
+            u32x2{pack2<Q>(s.o[0] * a.v_scale, s.o[1] * a.v_scale),
+                  pack2<Q>(s.o[2] * a.v_scale, s.o[3] * a.v_scale)};
         if (a.lse && lane == 0)
             a.lse[row * a.q_heads + h] = (s.top - kLift + __builtin_log2f(s.total)) * kLn2;
     }

@@ -829,3 +829,19 @@ def test_results_that_share_memory_are_refused():
         y, size = ref.rotate(q, pos, rope, False)
         f = size * 3 * 2.0 ** -24
         ref.assert_within(turned, y, y.abs() * 2.0 ** -8 + f * (1 + 2.0 ** -8), "queries")
+
+
+@pytest.mark.parametrize("vs", [2.0 ** -124, 2.0 ** 115])
+def test_value_scales_at_the_ends_of_fp32(vs):
+    """The scale of the values does not underflow on its way to the result, over long
+    contexts too, whose sums of weights are large."""
+    ctx, new = [30000, 7, 900, 1300], [1, 1, 300, 3]
+    shape = (1, 2100, 2, 16, 128, FP8)
+    with Step(shape, 8, ctx, new, torch.bfloat16, seed=3) as s:
+        # Values of 64 to 120, so that results are normal numbers of bf16.
+        vals = s.pool.view(1, 2100, 2, 2, 16, 128)[:, :, 1]
+        vals.copy_(torch.where(vals == 0xFF, vals, vals % 8 + 0x68))
+        for scale in (None, 0.0):                      # 0: sums of weights as large as can be
+            out, lse = s.batch.attend(0, s.q, lse=True, v_scale=vs, scale=scale)
+            torch.cuda.synchronize()
+            s.check_attend(0, s.q, f"scaled, {scale}", got=(out.to(F64) / vs, lse), scale=scale)
