@@ -201,15 +201,16 @@ __device__ inline void fit_queries(typename Mat<M>::v8 (&qf)[N], float* scale2, 
 }
 
 // Makes the scores' scale positive: queries change their sign with it, so that the
-// largest product is the largest score.  A scale of 0 becomes the least there is, with
-// which all scores are 0 and masked ones, -inf, stay what they are.
+// largest product is the largest score.  A scale of 0 becomes the least there is, 2^-149,
+// with which all scores are next to 0 (2^-21 at most) and masked ones, -inf, stay what
+// they are.
 template <typename V8, int N>
 __device__ inline void fit_scale(V8 (&qf)[N], float* scale2) {
     if (*scale2 < 0.0f)
 #pragma unroll
         for (int n = 0; n < N; ++n)
             qf[n] = __builtin_bit_cast(V8, __builtin_bit_cast(u32x4, qf[n]) ^ 0x80008000u);
-    *scale2 = fmaxf(fabsf(*scale2), 1.17549435e-38f);
+    *scale2 = fmaxf(fabsf(*scale2), 0x1p-149f);
 }
 
 // The softmax is computed in powers of two.  The running maximum is raised only when

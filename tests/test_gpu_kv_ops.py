@@ -845,3 +845,25 @@ def test_value_scales_at_the_ends_of_fp32(vs):
             out, lse = s.batch.attend(0, s.q, lse=True, v_scale=vs, scale=scale)
             torch.cuda.synchronize()
             s.check_attend(0, s.q, f"scaled, {scale}", got=(out.to(F64) / vs, lse), scale=scale)
+
+
+@pytest.mark.parametrize("m", [3, 150], ids=["rows", "tiles"])
+def test_a_scale_of_zero_with_products_as_large_as_they_come(m):
+    """All scores are 0 then, and below fp32's normal scales what the product makes of
+    them."""
+    ctx = [400]
+    with Step((1, 30, 2, 16, 128, BF16), 4, ctx, [m], torch.bfloat16, seed=5) as s:
+        used = s.pool.view(torch.bfloat16).view(30, 2, 2, 16, 128)
+        keys = used[:, 0]
+        keys.copy_(torch.where(keys.isfinite(), keys * 2.0 ** 58, keys))
+        q = s.q * 2.0 ** 58                            # products of 2^116 to 2^123
+        vals = ref.values(s.pool, s.shape)
+        for scale in (0.0, 2.0 ** -130, -(2.0 ** -130)):
+            out, lse = s.batch.attend(0, q, lse=True, scale=scale)
+            torch.cuda.synchronize()
+            # scale * log2(e) has a subnormal's bits: 2^-149 of 2^-130 at most.
+            o, l, mass, reach = ref.attend(vals, 0, s.tables, ctx, [m], q, scale=scale)
+            bo, bl = ref.attend_bounds(o, l, mass, reach, 128, 400, torch.bfloat16, BF16, 6.0)
+            extra = reach * 2.0 ** -19 + 2.0 ** 123 * 2.0 ** -148
+            ref.assert_within(lse, l, bl + extra, f"{scale}: lse")
+            ref.assert_within(out, o, bo + 2.1 * extra[..., None] * mass, f"{scale}: out")
