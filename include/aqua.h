@@ -679,9 +679,14 @@ typedef struct {
  * including each query's own position in `layer` of the pool: what aqua_kv_append
  * has written there, or a swap-in brought.  Whatever stands in the pool behind a
  * context, or at positions that a query must not see, has no influence, NaN
- * and infinity included.  Sums and statistics are fp32; the weights are
- * rounded to the 16-bit type that the matrix instructions take.  Results do not
- * depend on the order in which workgroups run. */
+ * and infinity included.  A value that is not finite and that a query does see leaves
+ * that element of its result not finite, infinite or NaN.  Sums and statistics are
+ * fp32; the weights are rounded to the 16-bit type that the matrix instructions take
+ * (fp16 on a 4-bit pool, else the queries'), and where at most 64 (new token, query
+ * head) pairs of a sequence share a KV head a second term holds what that rounding
+ * left, but for bf16 queries on a 4-bit pool.  Scores are fp32 too, in powers of two:
+ * results are defined for scores (scale * k_scale * q k) up to 2^24 in size.  Results do
+ * not depend on the order in which workgroups run. */
 AQUA_API aqua_status aqua_kv_attend(aqua_kv_batch_t batch, uint32_t layer,
                                     const aqua_kv_attend_args* args, void* stream);
 

@@ -867,3 +867,60 @@ def test_a_scale_of_zero_with_products_as_large_as_they_come(m):
             extra = reach * 2.0 ** -19 + 2.0 ** 123 * 2.0 ** -148
             ref.assert_within(lse, l, bl + extra, f"{scale}: lse")
             ref.assert_within(out, o, bo + 2.1 * extra[..., None] * mass, f"{scale}: out")
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("m", [2, 150], ids=["rows", "tiles"])
+def test_scores_as_large_as_the_header_has_them(m, kind):
+    """Scores up to 2^24 in size: each query's weight is all on the key that stands out
+    for it, and the log sum is that score."""
+    D, ctx = 64, [700]
+    shape = (1, 50, 1, 16, D, kind[0])
+    with Step(shape, 2, ctx, [m], kind[1], seed=5) as s:
+        q = torch.zeros_like(s.q)
+        q[:, 0, 0], q[:, 1, 0] = 4.0, -4.0
+        # Keys of one value: 1, and 3 at position 300; -2 at position 301.
+        k = torch.zeros(700, 1, D, dtype=kind[1], device="cuda")
+        k[:, 0, 0] = 1
+        k[300, 0, 0], k[301, 0, 0] = 3, -2
+        v = torch.randn(700, 1, D, device="cuda").to(kind[1])
+        one = aqua.KVBatch(s.kv, 2, 1, 700, 44)
+        one.set(s.tables, ctx, ctx)
+        one.append(0, k, v)
+        held = ref.cached(ref.values(s.pool, shape), 0, s.tables[0], 700)[1][0]
+        scale = 2.0 ** 20
+        out, lse = s.batch.attend(0, q, lse=True, scale=scale)
+        torch.cuda.synchronize()
+        # Scores of 12 * 2^20 (products of 3 and 4) and 8 * 2^20; a key's 4-bit rounding (a
+        # group of 0 and 3: half a step of 1/5, times 4) and log2(e)'s in fp32.
+        off = 0.4 if kind[0] == INT4 else 0.0
+        for h, at, want in ((0, 300, 12.0), (1, 301, 8.0)):
+            assert float((lse[:, h].to(F64) - want * scale).abs().max()) <= \
+                (want * 2.0 ** -21 + off) * scale
+            assert bool(((out[:, h].to(F64) - held[at]).abs() <=
+                         held[at].abs() * 2.0 ** -7 + 2.0 ** -24).all())
+
+
+@pytest.mark.parametrize("kind", [KINDS[0], KINDS[1], KINDS[3], KINDS[4]],
+                         ids=[KIND_IDS[i] for i in (0, 1, 3, 4)])
+@pytest.mark.parametrize("m", [1, 3, 150], ids=["one", "rows", "tiles"])
+def test_values_that_are_not_finite_and_seen(m, kind):
+    """An element of a value that every query sees and that is not finite leaves that
+    element of the results not finite, and the others as they are."""
+    pool_dtype, dt = kind
+    shape, ctx, d = (1, 60, 1, 16, 128, pool_dtype), [900], 37
+    with Step(shape, 4, ctx, [m], dt, seed=5) as s:
+        clean, clean_lse = s.batch.attend(0, s.q, lse=True)
+        block, slot = int(s.tables[0][20]), 3
+        if pool_dtype == INT4:
+            ref.codes_and_pairs(s.pool, shape)[1][0, block, 1, 0, slot, d // 32, 1] = float("inf")
+            hit = torch.arange(128, device="cuda") // 32 == d // 32
+        else:
+            row = s.pool.view(ref.TORCH[pool_dtype]).view(60, 2, 1, 16, 128)
+            row[block, 1, 0, slot, d] = float("nan") if pool_dtype == FP8 else -float("inf")
+            hit = torch.arange(128, device="cuda") == d
+        out, lse = s.batch.attend(0, s.q, lse=True)
+        torch.cuda.synchronize()
+        assert torch.equal(lse, clean_lse)
+        assert torch.equal(out[..., ~hit], clean[..., ~hit])
+        assert not bool(out[..., hit].isfinite().any())
