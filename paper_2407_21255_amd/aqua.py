@@ -458,6 +458,8 @@ def _csr(tables):
 # the 10 us that a small call costs its caller).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _cur_device = getattr(torch._C, "_cuda_getDevice", None)
+_capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing",
+                     torch.cuda.is_current_stream_capturing)
 
 
 def _stream_handle(stream) -> Optional[int]:
@@ -731,8 +733,10 @@ class KVBatch:
             raise AquaError(st, "aqua_kv_batch_create")
         self.handle = h
         self.pool = pool
+        self.device = pool.pool.device.index
         self.num_q_heads = num_q_heads
         self.head_dim = pool.desc.head_dim
+        self.num_layers, self.num_kv_heads = pool.desc.num_layers, pool.desc.num_kv_heads
         self.max_tokens = max_tokens
         self.tokens = 0
         pool._spaces.append(self)
@@ -759,34 +763,44 @@ class KVBatch:
             raise AquaError(AQUA_ERR_INVALID, "aqua_kv_batch_set")
         ctx32, fresh32 = ctx.astype(np.uint32), np.minimum(fresh, (1 << 32) - 1).astype(np.uint32)
         st = aqua_kv_batch_set(self.handle, len(ctx), _addr(ids), _addr(offs), _addr(ctx32),
-                               _addr(fresh32), _stream_handle(stream))
+                               _addr(fresh32), self._stream(stream))
         if st != AQUA_OK:
             raise AquaError(st, "aqua_kv_batch_set")
         self.tokens = int(fresh.sum())
-
-    def _check_layer(self, layer: int, what: str) -> None:
-        if not 0 <= layer < self.pool.desc.num_layers:   # (ctypes takes a number's low bits)
-            raise AquaError(AQUA_ERR_INVALID, what)
 
     @staticmethod
     def _no_gradients(what: str, *tensors) -> None:
         """The operators have no backward pass: a result that silently has no gradient
         would cut the caller's graph."""
-        if torch.is_grad_enabled():
-            for t in tensors:
-                if t is not None and t.requires_grad:
-                    raise AquaError(AQUA_ERR_INVALID, what + ", which makes no gradient, of a "
-                                    "tensor that requires one (detach it, or use torch.no_grad())")
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise AquaError(AQUA_ERR_INVALID, what + ", which makes no gradient, of a "
+                                "tensor that requires one (detach it, or use torch.no_grad())")
+
+    def _stream(self, stream) -> Optional[int]:
+        """A call's stream as a handle: unless given the current one of the pool's device,
+        which need not be the current device."""
+        if stream is None:
+            if _raw_stream is not None:
+                return _raw_stream(self.device) or None
+            stream = torch.cuda.current_stream(self.device)
+        return _stream_handle(stream)
+
+    def _stream_object(self, stream):
+        return torch.cuda.ExternalStream(stream, device=self.device) \
+            if isinstance(stream, int) else stream
 
     def _needed(self, stream) -> int:
         """Rows that a call's tensors have: the step's, or, for a call that is being
         captured, as many as a step can ever have."""
-        if stream is None:
-            capturing = torch.cuda.is_current_stream_capturing()
+        if stream is not None:
+            with torch.cuda.stream(self._stream_object(stream)):
+                capturing = _capturing()
+        elif _cur_device is None or _cur_device() != self.device:
+            with torch.cuda.device(self.device):
+                capturing = _capturing()
         else:
-            s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
-            with torch.cuda.stream(s):
-                capturing = torch.cuda.is_current_stream_capturing()
+            capturing = _capturing()
         return self.max_tokens if capturing else self.tokens
 
     def _stride(self, t: torch.Tensor, heads: int, rows: int, what: str) -> int:
@@ -798,25 +812,21 @@ class KVBatch:
             raise AquaError(AQUA_ERR_INVALID, what)
         return s[0] if n[0] > 1 else heads * D     # (a single row's stride says nothing)
 
-    @staticmethod
-    def _used(stream, *tensors) -> None:
+    def _used(self, stream, *tensors) -> None:
         """Tensors of torch's allocator that another than the current stream uses are
         not handed out again before it is done with them."""
-        if stream is None:
-            return
-        s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+        s = self._stream_object(stream)
         if s.cuda_stream != torch.cuda.current_stream(s.device).cuda_stream:
             for t in tensors:
                 if t is not None:
                     t.record_stream(s)
 
-    @staticmethod
-    def _result(stream, like: torch.Tensor, dtype=None) -> torch.Tensor:
+    def _result(self, stream, like: torch.Tensor, dtype=None) -> torch.Tensor:
         """A new tensor like `like` that a call on `stream` fills.  It is the memory of that
         stream: what the current one has let go may still be in use there."""
         if stream is None:   # (1.2 us; new_empty takes 1.8)
             return torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
-        s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+        s = self._stream_object(stream)
         current = torch.cuda.current_stream(like.device)
         with torch.cuda.stream(s):
             t = torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
@@ -832,9 +842,11 @@ class KVBatch:
         """aqua_kv_append.  ``rope``: float32 [positions, rotated part of a head], cosines
         and then sines.  Returns the rotated queries (``q_out``, which may be ``q``
         itself, or a new tensor), None without ``q``."""
-        name, H = "aqua_kv_append", self.pool.desc.num_kv_heads
-        self._check_layer(layer, name)
-        self._no_gradients(name, k, v, q, q_out, rope)
+        name, H = "aqua_kv_append", self.num_kv_heads
+        if not 0 <= layer < self.num_layers:   # (ctypes takes a number's low bits)
+            raise AquaError(AQUA_ERR_INVALID, name)
+        if torch.is_grad_enabled():
+            self._no_gradients(name, k, v, q, q_out, rope)
         dtype = _DTYPES.get(k.dtype)
         if dtype is None or v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
             raise AquaError(AQUA_ERR_INVALID, name)
@@ -859,10 +871,11 @@ class KVBatch:
                     or not rope.is_cuda:
                 raise AquaError(AQUA_ERR_INVALID, name)
             a.rope, a.rope_rows, a.rope_dim = rope.data_ptr(), rope.shape[0], rope.shape[1]
-        st = aqua_kv_append(self.handle, layer, a, _stream_handle(stream))
+        st = aqua_kv_append(self.handle, layer, a, self._stream(stream))
         if st != AQUA_OK:
             raise AquaError(st, name)
-        self._used(stream, k, v, q, q_out, rope)
+        if stream is not None:
+            self._used(stream, k, v, q, q_out, rope)
         return q_out
 
     def attend(self, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None,
@@ -872,8 +885,10 @@ class KVBatch:
         a contiguous float32 tensor [tokens, query heads] to fill; then (out, lse) is
         returned, else out."""
         name = "aqua_kv_attend"
-        self._check_layer(layer, name)
-        self._no_gradients(name, q, out, None if isinstance(lse, bool) else lse)
+        if not 0 <= layer < self.num_layers:
+            raise AquaError(AQUA_ERR_INVALID, name)
+        if torch.is_grad_enabled():
+            self._no_gradients(name, q, out, None if isinstance(lse, bool) else lse)
         dtype = _DTYPES.get(q.dtype)
         if dtype is None:
             raise AquaError(AQUA_ERR_INVALID, name)
@@ -896,10 +911,11 @@ class KVBatch:
             q_stride=stride, out_stride=self._stride(out, self.num_q_heads, rows, name), dtype=dtype,
             scale=self.head_dim ** -0.5 if scale is None else scale,
             k_scale=k_scale, v_scale=v_scale)
-        st = aqua_kv_attend(self.handle, layer, a, _stream_handle(stream))
+        st = aqua_kv_attend(self.handle, layer, a, self._stream(stream))
         if st != AQUA_OK:
             raise AquaError(st, name)
-        self._used(stream, q, out, lse)
+        if stream is not None:
+            self._used(stream, q, out, lse)
         return out if lse is None else (out, lse)
 
     def close(self) -> None:

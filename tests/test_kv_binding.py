@@ -25,13 +25,14 @@ def calls(monkeypatch):
         return aqua.AQUA_OK
 
     monkeypatch.setattr(aqua, "aqua_kv_batch_set", take)
-    monkeypatch.setattr(aqua, "_stream_handle", lambda stream: None)
+    monkeypatch.setattr(aqua, "_raw_stream", lambda device: 0)
     return seen
 
 
 def batch(layers=2):
     b = aqua.KVBatch.__new__(aqua.KVBatch)
     b.handle, b.num_q_heads, b.head_dim, b.max_tokens, b.tokens = None, 4, 128, 100, 0
+    b.device, b.num_layers, b.num_kv_heads = 0, layers, 2
     b.pool = types.SimpleNamespace(
         handle=None, _spaces=[b], desc=aqua.aqua_kv_desc(layers, 100, 2, 16, 128, aqua.AQUA_BF16))
     return b
@@ -107,6 +108,7 @@ def test_numbers_that_32_bits_do_not_hold(monkeypatch):
                 call()
             assert e.value.status == INVALID
     pool = batch().pool
+    pool.pool = torch.zeros(1)
     for args in ((4 + (1 << 32), 1, 1, 1), (4, 1 + (1 << 32), 1, 1), (4, 1, 1 + (1 << 32), 1),
                  (4, 1, 1, 1 + (1 << 32)), (4, -1, 1, 1)):
         with pytest.raises(aqua.AquaError) as e:
@@ -127,3 +129,36 @@ def test_tensors_that_require_a_gradient_are_refused():
         with pytest.raises(aqua.AquaError, match="gradient") as e:
             call(batch())
         assert e.value.status == INVALID
+
+
+def test_the_stream_is_the_pools_devices_current_one(calls, monkeypatch):
+    """... whichever device is the current one, as for torch's own operators."""
+    monkeypatch.undo()
+    streams, entered = [], []
+    monkeypatch.setattr(aqua, "_raw_stream", lambda device: 1000 + device)
+    monkeypatch.setattr(aqua, "_cur_device", lambda: 0)
+    monkeypatch.setattr(aqua, "aqua_kv_batch_set", lambda *a: streams.append(a[-1]) or aqua.AQUA_OK)
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    b = batch()
+    b.device = 1
+    b.set([np.array([1])], [1], [1])
+    b.set([np.array([1])], [1], [1], stream=7)
+    b.device = 0
+    b.set([np.array([1])], [1], [1])
+    assert streams == [1001, 7, 1000]
+
+    class Device:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            entered.append(self.device)
+
+        def __exit__(self, *exc):
+            pass
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(aqua, "_capturing", lambda: len(entered) > 0)
+    assert b._needed(None) == 1 and entered == []      # the current device: not asked for
+    b.device = 1
+    assert b._needed(None) == b.max_tokens and entered == [1]
