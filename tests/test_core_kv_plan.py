@@ -311,3 +311,20 @@ def test_room_for_the_batchs_blocks_takes_no_part_from_a_step(heads, D):
             assert np.array_equal(a[name], b[name]), (trial, name)
             assert len(a[name]) <= lim.get(name, 1 << 32)
         assert a["counts"]["slots"] <= lim["slots"]
+
+
+def test_the_longest_context():
+    """2^30 tokens in blocks of 1024: parts and their ends stay within 32 bits."""
+    most = 1 << 30
+    for H, Hq in ((1, 1), (8, 64)):
+        table = np.arange(most // 1024, dtype=np.int32)
+        pool, batch = (1, most // 1024, H, 1024, 64, INT4), (Hq, 1, 20, most // 1024)
+        st, lim = limits(pool, batch)
+        assert st == OK
+        for new in (1, 20):
+            st, p = plan(pool, batch, [table], [most], [new])
+            assert st == OK and p["counts"]["longest"] == most
+            _check_cover(pool, batch, [0], [most], [new], p, lim)
+            assert p["tokens"].tolist()[-1] == [most // 1024 - 1, most - 1]
+            n = np.concatenate([x[:, 6].astype(int) - x[:, 5] for x in (p["rows"], p["tiles"])])
+            assert int(n.max()) <= most * H // 256 + 512

@@ -924,3 +924,136 @@ def test_values_that_are_not_finite_and_seen(m, kind):
         assert torch.equal(lse, clean_lse)
         assert torch.equal(out[..., ~hit], clean[..., ~hit])
         assert not bool(out[..., hit].isfinite().any())
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=KIND_IDS)
+@pytest.mark.parametrize("D", [64, 256])
+def test_heads_of_64_and_256_split_long_contexts(D, kind):
+    """Contexts of so many parts that groups of a join's lanes share them, with a tile of 16
+    columns that is partly filled."""
+    ctx, new = [20001, 7, 9000, 4097], [1, 1, 100, 3]
+    shape = (1, 2200, 2, 16, D, kind[0])
+    with Step(shape, 10, ctx, new, kind[1], seed=3) as s:
+        s.check_attend(0, s.q, "splits")
+
+
+@pytest.mark.parametrize("kind", [KINDS[1], KINDS[3], KINDS[4]],
+                         ids=[KIND_IDS[i] for i in (1, 3, 4)])
+@pytest.mark.parametrize("T", [128, 1024])
+def test_large_blocks(T, kind):
+    ctx, new = [3000, 1, T, T + 1, 900], [1, 1, 2, 1, 200]
+    shape = (2, 40, 2, T, 128, kind[0])
+    with Step(shape, 8, ctx, new, kind[1], seed=T) as s:
+        s.check_attend(1, s.q, "large blocks")
+        before, rope = s.pool.clone(), ref.rope_table(3000, 128)
+        q = s.batch.append(1, s.k, s.v, q=s.q, rope=rope)
+        torch.cuda.synchronize()
+        # (What no context holds is NaN here, and compared bit for bit.)
+        check_append(s, 1, rope, False, before, q)
+
+
+@pytest.mark.parametrize("kind", [KINDS[1], KINDS[4]], ids=[KIND_IDS[1], KIND_IDS[4]])
+def test_very_many_query_heads(kind):
+    """More columns of one token than a workgroup takes."""
+    shape = (1, 40, 1, 16, 64, kind[0])
+    with Step(shape, 4099, [300, 20], [2, 1], kind[1], seed=4, poison=False) as s:
+        s.check_attend(0, s.q, "heads")
+        before, rope = s.pool.clone(), ref.rope_table(300, 64)
+        q = s.batch.append(0, s.k, s.v, q=s.q, rope=rope)
+        torch.cuda.synchronize()
+        check_append(s, 0, rope, False, before, q)
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16], ids=["f16", "bf16"])
+def test_append_int4_code_by_code(dt):
+    """Scales, bases and codes are the fp32 formulas' to the last bit, at values halfway
+    between two codes too."""
+    shape, n = (1, 40, 2, 16, 256, INT4), 512
+    with Step(shape, 2, [n], [n], dt, poison=False) as s:
+        gen = torch.Generator(device="cuda").manual_seed(3)
+        x = torch.randn(n, 2, 256, device="cuda", generator=gen)
+        x = x * 2.0 ** torch.randint(-12, 14, (n, 2, 1), device="cuda", generator=gen)
+        # Groups of steps p = 2^-3 ... 2^4 from -8 p to 7 p, at and between the codes: exact.
+        p = 2.0 ** torch.randint(-3, 5, (n // 2, 2, 8, 1), device="cuda", generator=gen)
+        half = torch.randint(-15, 14, (n // 2, 2, 8, 32), device="cuda", generator=gen) * 0.5 * p
+        half[..., 3:4], half[..., 17:18] = -8 * p, 7 * p
+        x[::2] = half.flatten(2)
+        x = x.to(dt)
+        v = x.flip(0).contiguous()
+        s.batch.append(0, x, v)
+        torch.cuda.synchronize()
+        words, pairs = ref.codes_and_pairs(s.pool, shape)
+        ids = torch.from_numpy(s.tables[0]).long().cuda()[:n // 16]
+        rows = lambda t: t[0, ids].permute(1, 0, 3, 2, *range(4, t.dim() - 1)).flatten(1, 2)
+        code, pair = rows(ref.codes(words)).cpu(), rows(pairs).cpu()     # [2, n, H, ...]
+        for which, t in ((0, x), (1, v)):
+            g = t.cpu().float().clamp(-16384, 16384).unflatten(-1, (8, 32))
+            lo, hi = g.amin(-1), g.amax(-1)
+            scale = ((hi - lo) / torch.full_like(lo, 15.0)).half()       # IEEE divisions
+            base = (lo - 16 * scale.float()).half()
+            assert torch.equal(pair[which][..., 0], scale)
+            assert torch.equal(pair[which][..., 1], base)
+            step = torch.where(scale > 0, scale.float(), torch.ones_like(lo))[..., None]
+            want = (((g - base.float()[..., None]) / step).round() - 16).clamp(0, 15)
+            assert torch.equal(code[which].unflatten(-1, (8, 32)).float(), want)
+            if which == 0:                                               # the exact groups
+                e = ((g.double() - base.double()[..., None]) / step.double())[::2]
+                assert int(((e - e.floor()) == 0.5).sum()) > 10000
+                assert torch.equal((e.round() - 16).clamp(0, 15).float(), want[::2])
+
+
+def test_a_replayed_append_writes_what_the_call_itself_would():
+    """Nothing where two tables hold a block that is written; and of a context that reaches
+    behind the rotation table, the tokens before its end."""
+    shape = (1, 60, 2, 16, 128, BF16)
+    n, R = 40, 64
+    # A table of 100 rows within a larger tensor, whose other rows would show.
+    rope = torch.cat([ref.rope_table(100, R), torch.full((60, R), 3.0, device="cuda")])
+    with Step(shape, 4, [90, 50], [20, 20], torch.bfloat16, poison=False,
+              limits=(2, n, 60)) as s:
+        out = torch.full_like(s.q, 7.0)
+        graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            s.batch.append(0, s.k, s.v, q=s.q, q_out=out, rope=rope[:100])
+        free = np.random.default_rng(1).permutation(60).astype(np.int32)
+        a, b = free[:12], free[12:24]
+        for turn in range(3):
+            say("turn", turn)
+            # Both sequences write block 5 of a's.
+            s.batch.set([a, a], [90, 90], [20, 20])
+            before = s.pool.clone()
+            out.fill_(7.0)
+            with pytest.raises(aqua.AquaError) as e:
+                s.batch.append(0, s.k, s.v, q=s.q, q_out=out, rope=rope[:100])
+            assert e.value.status == aqua.AQUA_ERR_DUPLICATE
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(s.pool, before) and bool((out == 7).all())
+            # Positions 75 .. 114 and, one step later, one sequence that ends before the table does.
+            for tables, ctx, new in (([a, b], [115, 33], [30, 10]), ([b], [100], [40])):
+                s.batch.set(tables, ctx, new)
+                if ctx[0] > 100:
+                    with pytest.raises(aqua.AquaError) as e:
+                        s.batch.append(0, s.k, s.v, q=s.q, q_out=out, rope=rope[:100])
+                    assert e.value.status == aqua.AQUA_ERR_INVALID
+                s.pool.fill_(0)
+                out.fill_(7.0)
+                graph.replay()
+                torch.cuda.synchronize()
+                pos = torch.from_numpy(ref.positions(ctx, new)).cuda()
+                blk, slot = ref.slots(tables, ctx, new, 16)
+                m, held = len(pos), s.pool.view(torch.bfloat16).view(60, 2, 2, 16, 128)
+                there = pos < 100
+                assert int(there.sum()) == min(m, m - (ctx[0] - 100))
+                for x, got in ((s.q, out[:m]), (s.k, held[blk, 0, :, slot])):
+                    y, size = ref.rotate(x[:m], pos.clamp(max=99), rope[:100], False)
+                    f = size * 3 * 2.0 ** -24
+                    bound = y.abs() * 2.0 ** -8 + f * (1 + 2.0 ** -8)
+                    ref.assert_within(got[there], y[there], bound[there], "rotated")
+                assert torch.equal(held[blk, 1, :, slot][there], s.v[:m][there])
+                assert bool((out[:m][~there] == 7).all()) and bool((out[m:] == 7).all())
+                # Nothing else: as many values as tokens have, all of them not 0 in the main.
+                held[blk[there], :, :, slot[there]] = 0
+                assert not bool(s.pool.any())
+        del graph
