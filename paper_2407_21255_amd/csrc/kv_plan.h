@@ -32,7 +32,11 @@ constexpr uint32_t tile_columns(uint32_t head_dim) { return head_dim > 128 ? 128
 constexpr uint32_t kRowsMostColumns = 64;
 
 // How a kernel's items are split into parts of at most `most` tokens (part_tokens):
-//   wide     workgroups that run at once;
+//   wide     workgroups that a round is counted as, for all head sizes: two a compute
+//            unit (rows) and one (tiles).  By the kernels' registers and LDS, a compute unit
+//            has room for three rows workgroups with heads of 128, three or four with
+//            64 and one with 256, and for one of tiles; what follows was measured with
+//            heads of 128;
 //   step     tokens that a workgroup takes in a step: parts are whole ones;
 //   fewest   tokens of a part that is worth a join;
 //   rounds   parts of split items are at most `wide` times this many workgroups, and so are

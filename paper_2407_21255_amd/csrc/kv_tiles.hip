@@ -42,7 +42,7 @@ struct Raw16 {
     }
     __device__ void clear(int i) { v[i] = u32x2{0, 0}; }
     template <typename M>
-    __device__ void keys_of(u32x4 (&out)[2], int) const {
+    __device__ void keys_of(u32x4 (&out)[2]) const {
         out[0] = k[0];
         out[1] = k[1];
     }
@@ -74,7 +74,7 @@ struct Raw<kFP8, D> {
     }
     __device__ void clear(int i) { v[i] = 0; }
     template <typename M>
-    __device__ void keys_of(u32x4 (&out)[2], int) const {
+    __device__ void keys_of(u32x4 (&out)[2]) const {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             out[i / 2][i % 2 * 2] = Mat<M>::template from_fp8<false>(k[i]);
@@ -111,7 +111,7 @@ struct Raw<kInt4, D> {
     }
     __device__ void clear(int i) { vp[i] = 0; }
     template <typename M>
-    __device__ void keys_of(u32x4 (&out)[2], int) const {
+    __device__ void keys_of(u32x4 (&out)[2]) const {
         const f16x2 s = __builtin_bit_cast(f16x2, pair_lo(kp, kp));
         const f16x2 b = __builtin_bit_cast(f16x2, pair_hi(kp, kp));
 #pragma unroll
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(2 * (int)tile_columns(D)) void tiles_kernel(const K
             const uint32_t n = threadIdx.x + i * kThreads;
             if (kUnits % kThreads && n >= kUnits) break;
             u32x4 kw[2];
-            raw[i].template keys_of<M>(kw, 0);
+            raw[i].template keys_of<M>(kw);
             const uint32_t row = n / (D / 16), piece = n % (D / 16) * 2;
             *reinterpret_cast<u32x4*>(&keys[buf][key_at<D>(row, piece)]) = kw[0];
             *reinterpret_cast<u32x4*>(&keys[buf][key_at<D>(row, piece + 1)]) = kw[1];
@@ -337,6 +337,11 @@ __global__ __launch_bounds__(2 * (int)tile_columns(D)) void tiles_kernel(const K
                     for (int r = 0; r < 16; ++r) acc[d][r] *= f;
             }
             const float off = top > -__builtin_inff() ? top - kLift : 0.0f;
+            // Weights are rounded once, to the products' type: a second term with what that
+            // leaves, as the rows kernel has it, would be half as many products again
+            // where these are what takes the time.  An 8192-token bf16 prompt is off by
+            // 0.0020 of its size against 64 bits, with weights in fp32 by 0.0015 (the
+            // result's own rounding to bf16).
             V8 pf[kRuns];
 #pragma unroll
             for (int kt = 0; kt < kRuns; ++kt) {
