@@ -644,23 +644,23 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 3) void rows_kernel(const KvAtte
         return;
     }
     const uint64_t row = seq.row + oc_all / G, h = head * G + oc_all % G;
-    // (The values' scale by itself: over the sum it may be too small for fp32.)
+    // (The values' scale by itself: over the sum it may be too small for fp32.  Only fp8
+    // pools have one.)
     const float norm = 1.0f / total;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] *= norm;
+    if (POOL == kFP8)
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] *= a.v_scale;
     uint8_t* out = a.out + 2 * (row * a.out_stride + h * D + od);
     if constexpr (E == 4) {
-        *reinterpret_cast<u32x2*>(out) =
-            u32x2{pack2<Q>(o[0] * a.v_scale, o[1] * a.v_scale),
-                  pack2<Q>(o[2] * a.v_scale, o[3] * a.v_scale)};
+        *reinterpret_cast<u32x2*>(out) = u32x2{pack2<Q>(o[0], o[1]), pack2<Q>(o[2], o[3])};
     } else {
 #pragma unroll
         for (int e = 0; e < E; e += 8)
             *reinterpret_cast<u32x4*>(out + 2 * e) =
-                u32x4{pack2<Q>(o[e] * a.v_scale, o[e + 1] * a.v_scale),
-                      pack2<Q>(o[e + 2] * a.v_scale, o[e + 3] * a.v_scale),
-                      pack2<Q>(o[e + 4] * a.v_scale, o[e + 5] * a.v_scale),
-                      pack2<Q>(o[e + 6] * a.v_scale, o[e + 7] * a.v_scale)};
+                u32x4{pack2<Q>(o[e], o[e + 1]), pack2<Q>(o[e + 2], o[e + 3]),
+                      pack2<Q>(o[e + 4], o[e + 5]), pack2<Q>(o[e + 6], o[e + 7])};
     }
     if (a.lse && od == 0)
         a.lse[row * a.q_heads + h] = (high - kLift + __builtin_log2f(total)) * kLn2;

@@ -413,16 +413,21 @@ __global__ __launch_bounds__(2 * (int)tile_columns(D)) void tiles_kernel(const K
         return;
     }
     const uint64_t row = seq.row + token, h = head * G + c % G;
-    // (The values' scale by itself: over the sum it may be too small for fp32.)
-    const float norm = 1.0f / sum, scale = a.v_scale;
+    // (The values' scale by itself: over the sum it may be too small for fp32.  Only fp8
+    // pools have one.)
+    const float norm = 1.0f / sum;
+#pragma unroll
+    for (int d = 0; d < kOut; ++d) acc[d] *= norm;
+    if (POOL == kFP8)
+#pragma unroll
+        for (int d = 0; d < kOut; ++d) acc[d] *= a.v_scale;
     uint8_t* out = a.out + 2 * (row * a.out_stride + h * D);
 #pragma unroll
     for (int d = 0; d < kOut; ++d)
 #pragma unroll
         for (int r = 0; r < 16; r += 4)
             *reinterpret_cast<u32x2*>(out + 2 * (d * 32 + r * 2 + half * 4)) =
-                u32x2{pack2<Q>(acc[d][r] * norm * scale, acc[d][r + 1] * norm * scale),
-                      pack2<Q>(acc[d][r + 2] * norm * scale, acc[d][r + 3] * norm * scale)};
+                u32x2{pack2<Q>(acc[d][r], acc[d][r + 1]), pack2<Q>(acc[d][r + 2], acc[d][r + 3])};
     if (a.lse && !half)
         a.lse[row * a.q_heads + h] = (top - kLift + __builtin_log2f(sum)) * kLn2;
 }
